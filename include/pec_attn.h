@@ -290,6 +290,109 @@ int pec_decode_splitkv_static(const pec_shape_t* shape, const void* q, const voi
                               int32_t n_splits, void* out, float* lse, void* stream);
 
 /*
+ * Keys and values in pages: the cache of a server that runs many sequences at once and hands out memory a page at a time.
+ * Token t of a sequence sits in slot t % page_size of page block_table[sequence][t / page_size], K and V alike.
+ *   k, v     : DEVICE bf16, element (page, slot, head, dim) at page * page_stride + slot * row_stride + head * head_stride +
+ *              dim (strides in elements, multiples of 8, the same for k and v), so that [pages, page_size, n_kv_heads, 128] and
+ *              [pages, n_kv_heads, page_size, 128] and parts of a larger allocation will do.  No two elements may overlap.
+ *   page_size: a power of two from 8 on; a page's slots and heads span less than 2^31 bytes.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t n_pages;     /* up to 2^31 - 1 */
+    int32_t page_size;
+    int32_t reserved;    /* 0 */
+    int64_t page_stride, row_stride, head_stride;
+} pec_paged_cache_t;
+
+/*
+ * The sequences of a call.  Sequence b has len_q = cu_seqlens_q[b+1] - cu_seqlens_q[b] new tokens (packed rows of q / k / v /
+ * out) and seqlens_k[b] tokens in all, the new ones the last of them, as in pec_attn_colocated: new token i is at position
+ * seqlens_k[b] - len_q + i.  All three arrays are DEVICE int32 and read when the call runs, so a captured call works on what
+ * they hold at each replay.
+ *   cu_seqlens_q [batch + 1], non-decreasing from 0; packed rows from cu_seqlens_q[batch] on belong to no sequence, and what
+ *                a call writes for each packed row is left as it was there (a padded batch).  Zero-length sequences are legal.
+ *   seqlens_k    [batch], at most table_len * page_size.
+ *   block_table  [batch, table_len] page numbers; those behind a sequence's last page are not looked at.  Sequences may share
+ *                pages; pages that new tokens go to belong to one sequence.
+ * Malformed values never lead out of bounds: offsets and lengths are clamped, keys of a page number outside the cache are read
+ * from some page of it, and nothing is written for one.
+ *   max_len_q, max_len_k: the caller's bounds on new tokens and tokens per sequence, 0 = unknown.  HINTS only: they choose how
+ *                the work is cut (so results for different hints may differ in rounding), never what is computed.
+ */
+typedef struct {
+    const int32_t* cu_seqlens_q;
+    const int32_t* seqlens_k;
+    const int32_t* block_table;
+    int32_t batch;
+    int32_t table_len;
+    int64_t total_q;     /* packed rows */
+    int64_t max_len_q, max_len_k;
+} pec_paged_batch_t;
+
+/*
+ * What happens to a row of 128 of a query or key head ahead of attention, in fp32 with one rounding to bf16 at the end:
+ *   1. norm, if there is a weight: x * weight / sqrt(mean(x^2) + eps);
+ *   2. rotation of the first rotary_dim values (R), if it is not 0: (a, b) -> (a cos - b sin, b cos + a sin) of the pairs
+ *      (i, i + R/2), or (2i, 2i + 1) with interleaved != 0, i < R/2, with the angles of the token's position p:
+ *      cos_sin[p][i] and cos_sin[p][R/2 + i].
+ *   q_weight, k_weight: DEVICE fp32 [128] or NULL; cos_sin: DEVICE fp32 [n_positions, rotary_dim], 16-byte aligned.
+ *   rotary_dim: 0 or a multiple of 16 up to 128.  Positions outside the table are taken at its nearer end.
+ */
+typedef struct {
+    const float* q_weight;
+    const float* k_weight;
+    const float* cos_sin;
+    int64_t n_positions;
+    int32_t rotary_dim;
+    int32_t interleaved;
+    float eps;           /* >= 0 */
+    int32_t reserved;    /* 0 */
+} pec_norm_rope_t;
+
+/*
+ * Norms of queries and keys per head and the rotation of positions, in one pass, for attention on contiguous keys (every other
+ * entry point of this header takes q and k as this call leaves them).
+ *   q [tokens, Hq, 128] with q_stride elements from token to token (0 = packed; a multiple of 8, at least Hq * 128), k likewise:
+ *   parts of one projection's output will do.  q_out [tokens, Hq, 128] and k_out [tokens, Hkv, 128], packed; q_out may be q and
+ *   k_out may be k where these are packed, else they must not overlap.  q or k NULL: only the other.
+ *   positions: DEVICE int32 [tokens], or NULL: token i is at pos0 + i (a ring member's q_off; then pos0 + tokens must not
+ *   exceed n_positions).
+ * shape: heads, head_dim and flags (0) count.  Memory-bound: every row is read once and written once.
+ */
+int pec_qk_norm_rope(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const int32_t* positions, int64_t pos0, int64_t tokens, void* q_out, void* k_out,
+                     void* stream);
+
+/*
+ * New tokens on their way into a paged cache: k (normed and rotated as norm_rope says, NULL = as it is) and v [total_q, Hkv,
+ * 128] are written to the slots of their positions, and q (optional) goes to q_out [total_q, Hq, 128] normed and rotated in the
+ * same launch.  Strides as in pec_qk_norm_rope; q_out may be a packed q.  A token whose position lies in no page (negative, or
+ * behind the block table's row) or whose page number is outside the cache is not stored; its q_out row is written.
+ * The cache must not overlap q, k and v.  Runs ahead of pec_attn_paged on the same stream, with the same batch.
+ */
+int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_t* cache,
+                     const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                     const void* v, int64_t v_stride, void* q_out, void* stream);
+
+/*
+ * Attention of every sequence's new tokens over its pages: what pec_attn_colocated computes for contiguous keys.  With
+ * causal != 0 query i of sequence b sees keys 0 ... seqlens_k[b] - len_q + i, otherwise all seqlens_k[b]; what the cache holds
+ * elsewhere -- behind a sequence's end, in positions that a row does not see -- reaches no result, NaN and infinities
+ * included.  One token per sequence (a decode step), a few (drafted tokens looked at together), a chunk of a prompt behind a
+ * cached prefix and whole prompts may be mixed.
+ *   q [total_q, Hq, 128] with q_stride elements from token to token (0 = packed); out [total_q, Hq, 128] in shape->out_dtype,
+ *   lse [Hq, total_q].  Rows without a visible key get out = 0, lse = -inf; a row whose weights are NaN gets NaN in both.
+ *   workspace: pec_paged_workspace_bytes() bytes, 16-byte aligned, whatever they hold; calls that may run at the same time need
+ *   one each.
+ * PEC_FLAG_SIMPLE_KERNEL runs the plain kernel (fp32 weights, a wavefront per row; needs no workspace).
+ */
+int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,
+                   int64_t q_stride, int causal, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q);
+
+/*
  * On-GPU halves of the head <-> sequence exchange of Ulysses-style sequence parallelism (section
  * "Sequence Parallelism of Megatron and Ulysses": an all-to-all turns "my sequence segment, all
  * heads" into "the whole sequence, my heads" before attention, and back afterwards).  bf16,

@@ -25,6 +25,7 @@ EXPORTS = (
     "pec_attn_chunk", "pec_attn_chunk_merge", "pec_attn_merge", "pec_finalize", "pec_sp_prefill",
     "pec_sp_workspace_bytes", "pec_sp_prefill_resumable", "pec_sp_resumable_workspace_bytes", "pec_sp_resumable_best_workspace_bytes", "pec_sp_prefill_num_steps", "pec_sp_prefill_step", "pec_decode_splitkv", "pec_ulysses_layout", "pec_sp_select_strategy", "pec_decode_default_splits",
     "pec_decode_workspace_bytes", "pec_decode_splitkv_static", "pec_mfma_probe", "pec_hbm_read_probe", "pec_attn_colocated", "pec_colocated_workspace_bytes", "pec_attn_varlen", "pec_varlen_workspace_bytes", "pec_status_string",
+    "pec_qk_norm_rope", "pec_paged_append", "pec_attn_paged", "pec_paged_workspace_bytes",
 )
 
 
@@ -44,6 +45,24 @@ class PecSpChoice(ctypes.Structure):
     _fields_ = [("attn_comm", ctypes.c_double * 2), ("attn_compute", ctypes.c_double * 2),
                 ("mlp_comm", ctypes.c_double * 2), ("mlp_compute", ctypes.c_double * 2),
                 ("seconds", (ctypes.c_double * 2) * 2), ("best_attn", ctypes.c_int32), ("best_mlp", ctypes.c_int32)]
+
+
+class PecPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class PecPagedBatch(ctypes.Structure):
+    _fields_ = [("cu_seqlens_q", ctypes.c_void_p), ("seqlens_k", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("table_len", ctypes.c_int32), ("total_q", ctypes.c_int64),
+                ("max_len_q", ctypes.c_int64), ("max_len_k", ctypes.c_int64)]
+
+
+class PecNormRope(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p),
+                ("n_positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 class PecError(RuntimeError):
@@ -96,6 +115,15 @@ def lib() -> ctypes.CDLL:
         L.pec_attn_colocated.restype = ci
         L.pec_colocated_workspace_bytes.argtypes = [sp, i32, i64, i64]
         L.pec_colocated_workspace_bytes.restype = sz
+        nr, pc, pb = ctypes.POINTER(PecNormRope), ctypes.POINTER(PecPagedCache), ctypes.POINTER(PecPagedBatch)
+        L.pec_qk_norm_rope.argtypes = [sp, nr, vp, i64, vp, i64, vp, i64, i64, vp, vp, vp]
+        L.pec_qk_norm_rope.restype = ci
+        L.pec_paged_append.argtypes = [sp, nr, pc, pb, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.pec_paged_append.restype = ci
+        L.pec_attn_paged.argtypes = [sp, pc, pb, vp, i64, ci, vp, vp, vp, sz, vp]
+        L.pec_attn_paged.restype = ci
+        L.pec_paged_workspace_bytes.argtypes = [sp, i32, i64]
+        L.pec_paged_workspace_bytes.restype = sz
         L.pec_hbm_read_probe.argtypes = [vp, sz, vp, vp]
         L.pec_hbm_read_probe.restype = ci
         L.pec_mfma_probe.argtypes = [vp, sz, i32, vp, sz, vp]
@@ -427,4 +455,188 @@ def pec_attn_varlen(q, k, v, cu_seqlens, max_seqlen: int, causal: bool = True, o
            lib().pec_attn_varlen(ctypes.byref(shp), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), batch, total,
                                  int(max_seqlen), int(bool(causal)), _ptr(out), _ptr(lse), _ptr(workspace),
                                  workspace.numel(), _stream(stream)))
+    return out, lse
+
+
+# ---- keys and values in pages
+
+class PagedCache:
+    """A server's key / value pages, laid out once: k, v [n_pages, page_size, Hkv, 128] bf16 on the GPU with a contiguous last
+    dim and any other strides (multiples of 8), the same for both; a cache laid out by heads is passed as its transpose(1, 2)."""
+
+    def __init__(self, k, v):
+        for t, n in ((k, "k"), (v, "v")):
+            if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4 and t.shape[3] == 128 and t.stride(3) == 1):
+                raise ValueError("%s must be a bfloat16 tensor [n_pages, page_size, heads, 128] on the GPU, its last dim contiguous" % n)
+        if k.shape != v.shape or k.stride() != v.stride() or k.device != v.device:
+            raise ValueError("k and v must have the same shape and strides, on the same GPU")
+        self.k, self.v, self.device, self.n_kv_heads = k, v, k.device, k.shape[2]
+        self.struct = PecPagedCache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], 0, k.stride(0), k.stride(1), k.stride(2))
+        self.ref = ctypes.byref(self.struct)
+
+
+class NormRope:
+    """What a model does to its query and key rows: norm weights (fp32 [128] or None) and the rotation's angles (cos_sin fp32
+    [n_positions, R], the R / 2 cosines of a position, then its sines; None: no rotation)."""
+
+    def __init__(self, cos_sin=None, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False):
+        for t, n in ((cos_sin, "cos_sin"), (q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None:
+                _require(t, torch.float32, n)
+        for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None and t.shape != (128,):
+                raise ValueError("%s must have 128 elements" % n)
+        if cos_sin is not None and cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [n_positions, rotary_dim]")
+        given = [t for t in (cos_sin, q_weight, k_weight) if t is not None]
+        if any(t.device != given[0].device for t in given):
+            raise ValueError("cos_sin and the weights must be on the same GPU")
+        self.tensors, self.device = (cos_sin, q_weight, k_weight), given[0].device if given else None
+        n_pos, rot = cos_sin.shape if cos_sin is not None else (0, 0)
+        self.struct = PecNormRope(_ptr(q_weight), _ptr(k_weight), _ptr(cos_sin), n_pos, rot, int(bool(interleaved)), float(eps), 0)
+        self.ref = ctypes.byref(self.struct)
+
+
+def _rows(t, name: str, device) -> int:
+    """Checks head rows [tokens, heads, 128] whose tokens may be apart; returns the stride between them."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.shape[2] == 128):
+        raise ValueError("%s must be a bfloat16 tensor [tokens, heads, 128] on the GPU" % name)
+    if t.device != device:
+        raise ValueError("%s is on another GPU" % name)
+    tokens, row, one = t.stride()
+    if t.numel() == 0:
+        return 0
+    if one != 1 or (t.shape[1] > 1 and row != 128):
+        raise ValueError("the heads of a token must be contiguous in %s" % name)
+    return tokens if t.shape[0] > 1 else 0
+
+
+def _require_on(t, dtype, name: str, device, shape=None):
+    _require(t, dtype, name)
+    if t.device != device:
+        raise ValueError("%s is on another GPU" % name)
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+
+
+class _OnDevice:
+    """The device of a call's tensors as the current one, where it is not already."""
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def _paged_batch(block_table, cu_seqlens_q, seqlens_k, total_q, max_len_q, max_len_k, device) -> PecPagedBatch:
+    for t, n in ((block_table, "block_table"), (cu_seqlens_q, "cu_seqlens_q"), (seqlens_k, "seqlens_k")):
+        _require_on(t, torch.int32, n, device)
+    batch = seqlens_k.numel()
+    if block_table.dim() != 2 or block_table.shape[0] != batch or cu_seqlens_q.numel() != batch + 1:
+        raise ValueError("block_table must be [batch, pages], cu_seqlens_q [batch + 1] and seqlens_k [batch]")
+    return PecPagedBatch(cu_seqlens_q.data_ptr(), seqlens_k.data_ptr(), block_table.data_ptr(), batch, block_table.shape[1],
+                         total_q, int(max_len_q), int(max_len_k))
+
+
+def pec_qk_norm_rope(q, k, norm_rope: NormRope, positions=None, pos0: int = 0, q_out=None, k_out=None, stream=None):
+    """q [T,Hq,128], k [T,Hkv,128] bf16 (parts of one projection's output will do) -> normed and rotated, packed.  `positions`
+    int32 [T], or None: token i is at pos0 + i.  q or k may be None; q_out may be a packed q, k_out a packed k."""
+    given = q if q is not None else k
+    if given is None:
+        raise ValueError("neither q nor k")
+    device, tokens = given.device, given.shape[0]
+    hq, hkv = q.shape[1] if q is not None else 1, k.shape[1] if k is not None else 1
+    strides = []
+    for t, n in ((q, "q"), (k, "k")):
+        strides.append(_rows(t, n, device) if t is not None else 0)
+        if t is not None and t.shape[0] != tokens:
+            raise ValueError("q and k must have the same number of tokens")
+    if norm_rope.device is not None and norm_rope.device != device:
+        raise ValueError("norm_rope is on another GPU")
+    if positions is not None:
+        _require_on(positions, torch.int32, "positions", device, (tokens,))
+    if q is not None and q_out is None:
+        q_out = torch.empty((tokens, hq, 128), dtype=torch.bfloat16, device=device)
+    if k is not None and k_out is None:
+        k_out = torch.empty((tokens, hkv, 128), dtype=torch.bfloat16, device=device)
+    if q is not None:
+        _require_on(q_out, torch.bfloat16, "q_out", device, q.shape)
+    if k is not None:
+        _require_on(k_out, torch.bfloat16, "k_out", device, k.shape)
+    both = q is not None and k is not None
+    # (heads of a call without q or k: any pair that divides)
+    shp = _shape_of(hq if both else max(hq, hkv), hkv if both else (max(hq, hkv) if q is None else 1), 128, torch.bfloat16, 0.0, 0)
+    with _OnDevice(device):
+        _check("pec_qk_norm_rope",
+               lib().pec_qk_norm_rope(ctypes.byref(shp), norm_rope.ref, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(positions),
+                                      int(pos0), tokens, _ptr(q_out) if q is not None else None,
+                                      _ptr(k_out) if k is not None else None, _stream(stream)))
+    return q_out, k_out
+
+
+def pec_paged_append(k, v, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, norm_rope: NormRope = None, q=None, q_out=None,
+                     stream=None):
+    """The new tokens' k (normed and rotated), v [T,Hkv,128] into their sequences' pages; q [T,Hq,128], if given, normed and
+    rotated into q_out, which is returned.  cu_seqlens_q [B+1], seqlens_k [B] (the new tokens among them) and block_table
+    [B, pages], all int32 on the GPU."""
+    device, (tokens, hkv, _) = cache.device, k.shape
+    k_stride, v_stride, q_stride = _rows(k, "k", device), _rows(v, "v", device), 0
+    if v.shape != k.shape or hkv != cache.n_kv_heads:
+        raise ValueError("k and v must have the same shape, with the heads of the cache")
+    hq = hkv
+    if q is not None:
+        q_stride, hq = _rows(q, "q", device), q.shape[1]
+        if q.shape[0] != tokens:
+            raise ValueError("q and k must have the same number of tokens")
+        if q_out is None:
+            q_out = torch.empty((tokens, hq, 128), dtype=torch.bfloat16, device=device)
+        _require_on(q_out, torch.bfloat16, "q_out", device, q.shape)
+    if norm_rope is not None and norm_rope.device is not None and norm_rope.device != device:
+        raise ValueError("norm_rope is on another GPU")
+    batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, tokens, 0, 0, device)
+    shp = _shape_of(hq, hkv, 128, torch.bfloat16, 0.0, 0)
+    with _OnDevice(device):
+        _check("pec_paged_append",
+               lib().pec_paged_append(ctypes.byref(shp), norm_rope.ref if norm_rope is not None else None, cache.ref,
+                                      ctypes.byref(batch), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_out),
+                                      _stream(stream)))
+    return q_out
+
+
+def pec_paged_workspace_bytes(n_q_heads: int, n_kv_heads: int, batch: int, total_q: int) -> int:
+    shp = _shape_of(n_q_heads, n_kv_heads, 128, torch.bfloat16, 0.0, 0)
+    return int(lib().pec_paged_workspace_bytes(ctypes.byref(shp), int(batch), int(total_q)))
+
+
+def pec_attn_paged(q, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, max_len_q: int = 0, max_len_k: int = 0,
+                   causal: bool = True, out_dtype=torch.bfloat16, scale: float = 0.0, flags: int = 0, out=None, lse=None,
+                   workspace=None, stream=None):
+    """Attention of every sequence's new tokens q [T,Hq,128] over its pages -> (out [T,Hq,128], lse [Hq,T]).  Arguments as for
+    pec_paged_append; max_len_q, max_len_k: the longest of the batch where the caller knows it, 0 otherwise (hints)."""
+    device = cache.device
+    q_stride = _rows(q, "q", device)
+    total, hq, d = q.shape
+    if out is None:
+        out = torch.empty((total, hq, d), dtype=out_dtype, device=device)
+    if lse is None:
+        lse = torch.empty((hq, total), dtype=torch.float32, device=device)
+    _require_on(out, out_dtype, "out", device, q.shape)
+    _require_on(lse, torch.float32, "lse", device, (hq, total))
+    batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, total, max_len_q, max_len_k, device)
+    shp = _shape_of(hq, cache.n_kv_heads, d, out_dtype, float(scale), int(flags))
+    with _OnDevice(device):
+        if workspace is None:
+            workspace = torch.empty(max(16, int(lib().pec_paged_workspace_bytes(ctypes.byref(shp), batch.batch, total))),
+                                    dtype=torch.uint8, device=device)
+        _require_on(workspace, torch.uint8, "workspace", device)
+        _check("pec_attn_paged",
+               lib().pec_attn_paged(ctypes.byref(shp), cache.ref, ctypes.byref(batch), _ptr(q), q_stride, int(bool(causal)),
+                                    _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream)))
     return out, lse

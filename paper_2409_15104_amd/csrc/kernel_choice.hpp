@@ -324,4 +324,10 @@ inline int64_t decode_default_ranges(int cu, int n_q_heads, int n_kv_heads, int6
     return std::max<int64_t>(1, std::min<int64_t>(per_cu, sk / 1024));
 }
 
+// Wavefronts per token of norm_rope_kernel, each with an equal part of the token's `rows` head rows, four of them at a time.
+inline int norm_rope_parts(int cu, int64_t tokens, int rows) {
+    const int64_t quads = (rows + 3) / 4, wanted = ((int64_t)cu * 16 + tokens - 1) / std::max<int64_t>(1, tokens);
+    return (int)std::max<int64_t>(1, std::min(quads, wanted));
+}
+
 }  // namespace pec

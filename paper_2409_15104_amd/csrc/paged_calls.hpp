@@ -1,0 +1,194 @@
+// C-ABI host side of the paged cache: argument validation and launches of pec_qk_norm_rope, pec_paged_append and
+// pec_attn_paged.  Part of pec_attn.hip.
+#pragma once
+
+namespace {
+
+// Elements between tokens, from an argument that may be 0 for packed; negative: not one.
+int64_t token_stride(int64_t stride, int heads) {
+    const int64_t packed = (int64_t)heads * kHeadDim;
+    if (stride == 0) return packed;
+    return stride >= packed && stride % 8 == 0 && stride <= ((int64_t)1 << 40) ? stride : -1;
+}
+
+int check_cache(const pec_shape_t* s, const pec_paged_cache_t* c, PagedKv* out) {
+    if (!c || !c->k || !c->v || c->n_pages <= 0 || c->page_size <= 0 || c->reserved != 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (c->page_size < 8 || (c->page_size & (c->page_size - 1)) != 0 || c->n_pages > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
+    if (misaligned(c->k) || misaligned(c->v) || ((c->page_stride | c->row_stride | c->head_stride) & 7)) return PEC_ERR_MISALIGNED;
+    const int64_t most = (int64_t)1 << 30;      // elements inside a page, 2^31 bytes
+    if (c->row_stride < kHeadDim || c->row_stride > most || (s->n_kv_heads > 1 && (c->head_stride < kHeadDim || c->head_stride > most)) ||
+        c->page_stride < 0 || c->page_stride > ((int64_t)1 << 45) || (c->n_pages > 1 && c->page_stride < kHeadDim))
+        return PEC_ERR_INVALID_ARGUMENT;
+    const int64_t head_stride = s->n_kv_heads > 1 ? c->head_stride : 0;
+    if ((c->page_size - 1) * c->row_stride + (s->n_kv_heads - 1) * head_stride + kHeadDim > most) return PEC_ERR_UNSUPPORTED;
+    out->k = static_cast<unsigned char*>(c->k);
+    out->v = static_cast<unsigned char*>(c->v);
+    out->page_b = c->page_stride * 2;
+    out->row_b = (uint32_t)(c->row_stride * 2);
+    out->head_b = (uint32_t)(head_stride * 2);
+    out->last_page = (uint32_t)(c->n_pages - 1);
+    out->log_page = 0;
+    while ((1 << out->log_page) < c->page_size) ++out->log_page;
+    return PEC_OK;
+}
+
+int check_batch(const pec_paged_batch_t* b, int page_size, PagedBatch* out) {
+    if (!b || b->batch < 0 || b->total_q < 0 || b->table_len < 0 || b->max_len_q < 0 || b->max_len_k < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (b->total_q > kMaxRows) return PEC_ERR_UNSUPPORTED;
+    if (b->batch > 0 && b->total_q > 0) {
+        if (!b->cu_seqlens_q || !b->seqlens_k || (b->table_len > 0 && !b->block_table)) return PEC_ERR_INVALID_ARGUMENT;
+        if ((reinterpret_cast<uintptr_t>(b->cu_seqlens_q) | reinterpret_cast<uintptr_t>(b->seqlens_k) |
+             reinterpret_cast<uintptr_t>(b->block_table)) & 3u)
+            return PEC_ERR_MISALIGNED;
+    }
+    out->cu_q = b->cu_seqlens_q;
+    out->len_k = b->seqlens_k;
+    out->table = b->block_table;
+    out->batch = b->batch;
+    out->table_len = b->table_len;
+    out->total_q = (int32_t)b->total_q;
+    out->max_keys = (int32_t)std::min<int64_t>((int64_t)b->table_len * page_size, kMaxRows);
+    return PEC_OK;
+}
+
+int check_norm_rope(const pec_norm_rope_t* n, NormRopeParams* p) {
+    if (!n) return PEC_OK;      // nothing is done to the rows
+    if (!(n->eps >= 0.f) || n->n_positions < 0 || n->rotary_dim < 0 || n->reserved != 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (n->rotary_dim % 16 != 0 || n->rotary_dim > kHeadDim || n->n_positions > kMaxRows) return PEC_ERR_UNSUPPORTED;
+    if (n->rotary_dim > 0 && (!n->cos_sin || n->n_positions == 0)) return PEC_ERR_INVALID_ARGUMENT;
+    if (((reinterpret_cast<uintptr_t>(n->q_weight) | reinterpret_cast<uintptr_t>(n->k_weight)) & 3u) || misaligned(n->cos_sin))
+        return PEC_ERR_MISALIGNED;
+    p->q_weight = n->q_weight;
+    p->k_weight = n->k_weight;
+    p->table = n->cos_sin;
+    p->n_positions = (int32_t)n->n_positions;
+    p->rotary = n->rotary_dim;
+    p->interleaved = n->interleaved != 0;
+    p->eps = n->eps;
+    return PEC_OK;
+}
+
+template <bool NORM, bool APPEND>
+void launch_norm_rope(const NormRopeParams& p, dim3 grid, hipStream_t st) {
+    const dim3 threads(kNormRopeThreads);
+    if (p.rotary == 0)
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNone, APPEND>), grid, threads, 0, st, p);
+    else if (p.interleaved)
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNext, APPEND>), grid, threads, 0, st, p);
+    else if (p.rotary == kHeadDim)
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsFar, APPEND>), grid, threads, 0, st, p);
+    else
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsHalf, APPEND>), grid, threads, 0, st, p);
+}
+
+int launch_norm_rope(NormRopeParams& p, bool append, hipStream_t st) {
+    const int rows = p.n_q_heads + (append ? 2 : 1) * p.n_kv_heads;
+    p.parts = norm_rope_parts(compute_units(), p.tokens, rows);
+    const int64_t waves = (int64_t)p.tokens * p.parts;
+    const int64_t blocks = (waves + kNormRopeThreads / 64 - 1) / (kNormRopeThreads / 64);
+    if (blocks > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks);
+    const bool norm = p.q_weight || p.k_weight;
+    if (append && norm) launch_norm_rope<true, true>(p, grid, st);
+    else if (append) launch_norm_rope<false, true>(p, grid, st);
+    else if (norm) launch_norm_rope<true, false>(p, grid, st);
+    else launch_norm_rope<false, false>(p, grid, st);
+    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pec_qk_norm_rope(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const int32_t* positions, int64_t pos0, int64_t tokens, void* q_out, void* k_out,
+                     void* stream) {
+    if (int rc = check_shape(shape, nullptr)) return rc;
+    if (shape->flags != 0) return PEC_ERR_UNSUPPORTED;
+    NormRopeParams p{};
+    if (!norm_rope || tokens < 0 || pos0 < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (int rc = check_norm_rope(norm_rope, &p)) return rc;
+    if (tokens > kMaxRows) return PEC_ERR_UNSUPPORTED;
+    if (tokens == 0) return PEC_OK;
+    if ((!q && !k) || (q && !q_out) || (k && !k_out)) return PEC_ERR_INVALID_ARGUMENT;
+    if (!positions && p.rotary > 0 && pos0 + tokens > p.n_positions) return PEC_ERR_INVALID_ARGUMENT;
+    p.q_stride = token_stride(q_stride, shape->n_q_heads);
+    p.k_stride = token_stride(k_stride, shape->n_kv_heads);
+    if ((q && p.q_stride < 0) || (k && p.k_stride < 0)) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(q) || misaligned(k) || misaligned(q_out) || misaligned(k_out) || (reinterpret_cast<uintptr_t>(positions) & 3u))
+        return PEC_ERR_MISALIGNED;
+    p.q = static_cast<const __bf16*>(q);
+    p.k = static_cast<const __bf16*>(k);
+    p.q_out = static_cast<__bf16*>(q_out);
+    p.k_out = static_cast<__bf16*>(k_out);
+    p.positions = positions;
+    p.pos0 = pos0;
+    p.tokens = (int32_t)tokens;
+    p.n_q_heads = q ? shape->n_q_heads : 0;
+    p.n_kv_heads = k ? shape->n_kv_heads : 0;
+    return launch_norm_rope(p, false, static_cast<hipStream_t>(stream));
+}
+
+int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_t* cache,
+                     const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                     const void* v, int64_t v_stride, void* q_out, void* stream) {
+    if (int rc = check_shape(shape, nullptr)) return rc;
+    if (shape->flags != 0) return PEC_ERR_UNSUPPORTED;
+    NormRopeParams p{};
+    if (int rc = check_cache(shape, cache, &p.cache)) return rc;
+    if (int rc = check_batch(batch, cache->page_size, &p.batch)) return rc;
+    if (int rc = check_norm_rope(norm_rope, &p)) return rc;
+    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
+    if (!k || !v || (q && !q_out)) return PEC_ERR_INVALID_ARGUMENT;
+    p.q_stride = token_stride(q_stride, shape->n_q_heads);
+    p.k_stride = token_stride(k_stride, shape->n_kv_heads);
+    p.v_stride = token_stride(v_stride, shape->n_kv_heads);
+    if ((q && p.q_stride < 0) || p.k_stride < 0 || p.v_stride < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_out)) return PEC_ERR_MISALIGNED;
+    p.q = static_cast<const __bf16*>(q);
+    p.k = static_cast<const __bf16*>(k);
+    p.v = static_cast<const __bf16*>(v);
+    p.q_out = static_cast<__bf16*>(q_out);
+    p.tokens = (int32_t)batch->total_q;
+    p.n_q_heads = q ? shape->n_q_heads : 0;
+    p.n_kv_heads = shape->n_kv_heads;
+    return launch_norm_rope(p, true, static_cast<hipStream_t>(stream));
+}
+
+size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q) {
+    if (!shape || shape->n_q_heads <= 0 || shape->n_kv_heads <= 0 || batch < 0 || total_q < 0) return 0;
+    return 256;
+}
+
+int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,
+                   int64_t q_stride, int causal, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    float scale;
+    if (int rc = check_shape(shape, &scale)) return rc;
+    if (shape->flags & ~(uint32_t)PEC_FLAG_SIMPLE_KERNEL) return PEC_ERR_UNSUPPORTED;
+    PagedAttnParams p{};
+    if (int rc = check_cache(shape, cache, &p.cache)) return rc;
+    if (int rc = check_batch(batch, cache->page_size, &p.batch)) return rc;
+    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
+    if (!q || !out || !lse) return PEC_ERR_INVALID_ARGUMENT;
+    p.q_stride = token_stride(q_stride, shape->n_q_heads);
+    if (p.q_stride < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(q) || misaligned(out) || misaligned(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return PEC_ERR_MISALIGNED;
+    const bool simple = (shape->flags & PEC_FLAG_SIMPLE_KERNEL) != 0;
+    if (!simple && (!workspace || workspace_bytes < pec_paged_workspace_bytes(shape, batch->batch, batch->total_q))) return PEC_ERR_WORKSPACE;
+    p.q = static_cast<const __bf16*>(q);
+    p.out = out;
+    p.lse = lse;
+    p.n_q_heads = shape->n_q_heads;
+    p.n_kv_heads = shape->n_kv_heads;
+    p.group = shape->n_q_heads / shape->n_kv_heads;
+    p.causal = causal != 0;
+    p.out_f32 = shape->out_dtype == PEC_F32;
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t rows = batch->total_q * shape->n_q_heads;
+    hipLaunchKernelGGL(paged_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p);
+    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
+
+}  // extern "C"

@@ -22,6 +22,8 @@
 #include "fwd_kernel_il.hpp"
 #include "fwd_split_kernel.hpp"
 #include "kernel_choice.hpp"
+#include "norm_rope_kernel.hpp"
+#include "paged_simple_kernel.hpp"
 #include "probes.hpp"
 
 namespace {
@@ -928,3 +930,5 @@ const char* pec_status_string(int status) {
 }
 
 }  // extern "C"
+
+#include "paged_calls.hpp"
