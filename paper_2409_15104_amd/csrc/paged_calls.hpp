@@ -51,6 +51,21 @@ int check_batch(const pec_paged_batch_t* b, int page_size, PagedBatch* out) {
     return PEC_OK;
 }
 
+// Workspace of pec_attn_paged: the pieces' O and LSE, two slots for each span of either variant of paged_step_kernel, and the
+// steps ahead of every sequence.
+struct PagedLayout {
+    size_t off_lse, off_prefix, bytes;
+};
+PagedLayout paged_layout(int cu, int32_t batch) {
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const size_t slot_rows = (size_t)cu * kPagedWaves1 * 2 * 32;
+    PagedLayout l;
+    l.off_lse = slot_rows * kHeadDim * sizeof(float);
+    l.off_prefix = up(l.off_lse + slot_rows * sizeof(float));
+    l.bytes = up(l.off_prefix + ((size_t)batch + 1) * sizeof(int32_t));
+    return l;
+}
+
 int check_norm_rope(const pec_norm_rope_t* n, NormRopeParams* p) {
     if (!n) return PEC_OK;      // nothing is done to the rows
     if (!(n->eps >= 0.f) || n->n_positions < 0 || n->rotary_dim < 0 || n->reserved != 0) return PEC_ERR_INVALID_ARGUMENT;
@@ -157,7 +172,7 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
 
 size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q) {
     if (!shape || shape->n_q_heads <= 0 || shape->n_kv_heads <= 0 || batch < 0 || total_q < 0) return 0;
-    return 256;
+    return paged_layout(compute_units(), batch).bytes;
 }
 
 int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,
@@ -186,8 +201,36 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t rows = batch->total_q * shape->n_q_heads;
-    hipLaunchKernelGGL(paged_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p);
+    if (simple) {
+        const int64_t rows = batch->total_q * shape->n_q_heads;
+        hipLaunchKernelGGL(paged_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p);
+        return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    }
+    if (batch->batch > kPagedChunks * 64) return PEC_ERR_UNSUPPORTED;
+    const int cu = std::max(8, compute_units() & ~7);
+    const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
+    const int nt = len_q * p.group <= 32 ? 1 : 2;
+    // every tile step has a number
+    const int64_t row_tiles = batch->total_q * p.group / (32 * nt) + batch->batch;
+    if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) * p.n_kv_heads > 2147483647.0) return PEC_ERR_UNSUPPORTED;
+    const PagedLayout l = paged_layout(compute_units(), batch->batch);
+    char* const ws = static_cast<char*>(workspace);
+    PagedStepParams s{};
+    s.a = p;
+    s.part_out = reinterpret_cast<float*>(ws);
+    s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+    s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
+    s.min_span = 2;
+    s.most_rows = 0x7fffffff;
+    s.n_spans = cu * (nt == 1 ? kPagedWaves1 : kPagedWaves2);
+    if (nt == 1)
+        hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
+    else
+        hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    const int64_t per_seq = std::min<int64_t>(16, (len_q * p.group + 32 * nt - 1) / (32 * nt));
+    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)std::min(batch->batch, 4096), (unsigned)shape->n_q_heads, (unsigned)per_seq),
+                       dim3(kPagedMergeThreads), 0, st, s, 32 * nt);
     return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
 }
 

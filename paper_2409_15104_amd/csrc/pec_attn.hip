@@ -24,6 +24,7 @@
 #include "kernel_choice.hpp"
 #include "norm_rope_kernel.hpp"
 #include "paged_simple_kernel.hpp"
+#include "paged_step_kernel.hpp"
 #include "probes.hpp"
 
 namespace {
