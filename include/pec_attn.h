@@ -354,7 +354,7 @@ typedef struct {
 /*
  * Norms of queries and keys per head and the rotation of positions, in one pass, for attention on contiguous keys (every other
  * entry point of this header takes q and k as this call leaves them).
- *   q [tokens, Hq, 128] with q_stride elements from token to token (0 = packed; a multiple of 8, at least Hq * 128), k likewise:
+ *   q [tokens, Hq, 128] with q_stride elements from token to token (0 = packed; a multiple of 8, from Hq * 128 to 2^25), k likewise:
  *   parts of one projection's output will do.  q_out [tokens, Hq, 128] and k_out [tokens, Hkv, 128], packed; q_out may be q and
  *   k_out may be k where these are packed, else they must not overlap.  q or k NULL: only the other.
  *   positions: DEVICE int32 [tokens], or NULL: token i is at pos0 + i (a ring member's q_off; then pos0 + tokens must not

@@ -44,7 +44,8 @@ struct WorkItem {        // one (sequence, query tile) of a packed or colocated 
     int32_t qtile;       // query tile; negative: keys k0 ... of a one-token (decode) sequence, one range for each of the
                          // item's work units (as many per KV head as it has query heads)
     int32_t slot;        // where the first range's partial result goes
-    int32_t pad[2];
+    int32_t pad[2];      // paged batch: the item's keys begin here, and end there (k0 is the sequence's row of the block table then,
+                         // slot the first of its partial results, or -1: it has all keys that it sees)
 };
 static_assert(sizeof(WorkItem) == 32, "fwd_il_kernel fetches work items as eight words");
 
@@ -118,6 +119,11 @@ struct FwdParams {
     struct SplitSeq* split_seqs;
     int32_t* n_split;
     uint64_t mark;
+    // keys and values in pages (fwd_il_kernel<kFwdPaged>; paged_common.hpp): k and v are the caches
+    const int32_t* table;
+    int64_t page_b;
+    uint32_t row_b, head_b, last_page;
+    int32_t log_page, table_len;
 };
 struct SplitSeq {        // a one-token sequence whose keys are cut into ranges
     int32_t seq, slot0, n_ranges, pad;

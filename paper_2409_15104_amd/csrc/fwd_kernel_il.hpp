@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "paged_common.hpp"
 
 namespace pec {
 
@@ -55,18 +56,20 @@ __device__ __forceinline__ void scale_acc_in_place(f32x16 (&o)[4], float a) {
         for (int r = 0; r < 16; ++r) asm volatile("v_mul_f32 %0, %0, %1" : "+v"(o[dt][r]) : "v"(a));
 }
 
-// Four instances, so that each carries only its own bookkeeping through the (register-starved) work-item code:
+// Five instances, so that each carries only its own bookkeeping through the (register-starved) work-item code:
 // kFwdDense -- one call = one problem, work items dealt in fixed rounds (ring step, fused merge, key splits, the
 // plain sweep); kFwdSweep -- the resumable sweep (progress table, stop word, state of stopped items);
 // kFwdList -- device-built work lists (packed and colocated batch), work items drawn at run time;
 // kFwdSpan -- the resumable sweep as one span of tile steps per workgroup: the items, one after the other, are cut wherever a
-// workgroup's equal share ends, and span_merge_kernel merges the pieces of an item.
-enum { kFwdDense = 0, kFwdSweep = 1, kFwdList = 2, kFwdSpan = 3 };
+// workgroup's equal share ends, and span_merge_kernel merges the pieces of an item;
+// kFwdPaged -- a work list over keys and values in pages: an item is a sequence's query tile and a range of its keys.
+enum { kFwdDense = 0, kFwdSweep = 1, kFwdList = 2, kFwdSpan = 3, kFwdPaged = 4 };
 
 template <int MODE>
 __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     constexpr bool kSweep = MODE == kFwdSweep;
-    constexpr bool kList = MODE == kFwdList;
+    constexpr bool kPaged = MODE == kFwdPaged;
+    constexpr bool kList = MODE == kFwdList || kPaged;
     constexpr bool kSpan = MODE == kFwdSpan;
     constexpr bool kStops = kSweep || kSpan;
     constexpr bool kAhead = !kStops;   // the next item's first loads go out before this item's results
@@ -93,7 +96,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     const int n_items_eff = kList ? min(*p.n_work, p.n_items) : p.n_items;
     const int log_heads = kStops ? 0 : p.log_heads;
     // work units per item and KV head: lists hold tiles of 256 positions, cut further inside this kernel
-    const int units = kList ? p.group : p.group >> log_heads;
+    const int units = kList && !kPaged ? p.group : p.group >> log_heads;
     const WorkOrder order(n_items_eff, units, p.n_kv_heads);
     const int64_t per_xcd = order.count;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -183,6 +186,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
         int logical, sq, sk, delta, row0, rw0, blk_last, kvh;
         int64_t kv_tok0, q_off0, q_stride, o_off0, lse_off0;
         bool part;      // a key range whose result is a partial one
+        int seq;        // row of the block table (paged)
     };
     const int64_t packed_stride = (int64_t)p.n_q_heads * kHeadDim;
     auto list_geometry = [&](int logical, const WorkItem& w) {
@@ -190,6 +194,29 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
         g.logical = logical;
         g.kvh = logical / order.per_kvh;
         const int rem = logical % order.per_kvh;
+        if constexpr (kPaged) {      // items are tiles of (256 >> log_heads) positions, a unit for each set of heads
+            const int u = rem % units, bm = BM >> log_heads;
+            const int head = g.kvh * p.group + (u << log_heads) + (wave >> (3 - log_heads));
+            g.seq = w.k0;
+            g.kv_tok0 = w.pad[0];
+            g.sk = w.pad[1] - w.pad[0];
+            g.sq = w.len_q;
+            g.delta = w.len_k - w.len_q - w.pad[0];
+            g.part = w.slot >= 0;
+            g.row0 = w.qtile * bm;
+            g.rw0 = g.row0 + ((wave << 5) & (bm - 1));
+            g.q_stride = p.q_row_stride;
+            g.q_off0 = w.q0 * p.q_row_stride + (int64_t)head * kHeadDim;
+            if (g.part) {            // partial results: 256 rows for each unit of an item
+                g.lse_off0 = ((int64_t)w.slot * p.n_kv_heads + g.kvh) * units * BM + (int64_t)u * BM + (wave << 5) - g.rw0;
+                g.o_off0 = g.lse_off0 * kHeadDim;
+            } else {
+                g.lse_off0 = (int64_t)head * p.lse_stride + w.q0;
+                g.o_off0 = w.q0 * packed_stride + (int64_t)head * kHeadDim;
+            }
+            g.blk_last = min(g.sq, g.row0 + bm) - 1;
+            return g;
+        }
         const int u = rem % units;
         g.sk = w.len_k;
         g.kv_tok0 = w.k0;
@@ -312,6 +339,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     int out_f32 = p.out_f32;
     const float* acc_in = p.acc_in;
     float* acc_out = p.acc_out;
+    int64_t o_stride = 0;      // paged: between rows of the results
     int seg_done = 0;          // resumable sweep: key segments this item has behind it
     int tile_end = 0, piece_slot = 0;      // spans: the piece in hand ends here; its slot; whether it is a whole item
     bool whole = false;
@@ -333,6 +361,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             lse_ptr = p.part_lse;
             out_f32 = 1;
         }
+        if constexpr (kPaged) o_stride = g.part ? kHeadDim : packed_stride;
     } else {
         const int unit = dense_unit(round0);
         if (unit < 0) return;
@@ -349,7 +378,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
         g.delta -= (int)g.kv_tok0;
     }
     const int sq = g.sq, sk = g.sk, delta = g.delta, row0 = g.row0, rw0 = g.rw0;
-    int64_t q_stride = g.q_stride, o_off0 = g.o_off0, lse_off0 = g.lse_off0;
+    int64_t q_stride = kPaged ? o_stride : g.q_stride, o_off0 = g.o_off0, lse_off0 = g.lse_off0;
     const int causal = p.causal;
     const int wave_last = rw0 + 31;
     int n_tiles = tiles_of(g);
@@ -366,7 +395,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     n_act = max(n_act, n_full);
     if (rw0 >= sq) n_full = n_act = 0;   // a wavefront without a valid row only helps loading tiles
 
-    const uint32_t kv_stride_b = (uint32_t)p.n_kv_heads * kHeadDim * 2;   // bytes per token
+    const uint32_t kv_stride_b = kPaged ? p.row_b : (uint32_t)p.n_kv_heads * kHeadDim * 2;   // bytes per token
     auto kv_base = [&](const __bf16* kv, const Geo& of) {
         return reinterpret_cast<const unsigned char*>(kv) + (of.kv_tok0 * p.n_kv_heads + of.kvh) * (int64_t)(kHeadDim * 2);
     };
@@ -426,9 +455,9 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     // further (same swizzle, since 32 is a multiple of both swizzle periods)
     uint32_t ldk_off0, ldv_off0;
     {
-        const int key = 4 * wave + ld_row;
-        ldk_off0 = (uint32_t)key * kv_stride_b + (uint32_t)(ld_pos ^ (key & 15)) * 16u;
-        ldv_off0 = (uint32_t)key * kv_stride_b + (uint32_t)((((ld_pos >> 2) ^ (key & 3)) << 2) | (ld_pos & 3)) * 16u;
+        const int key = 4 * wave + ld_row, from = kPaged ? ld_row : key;      // (the base of a paged block is its first key's row)
+        ldk_off0 = (uint32_t)from * kv_stride_b + (uint32_t)(ld_pos ^ (key & 15)) * 16u;
+        ldv_off0 = (uint32_t)from * kv_stride_b + (uint32_t)((((ld_pos >> 2) ^ (key & 3)) << 2) | (ld_pos & 3)) * 16u;
     }
     const uint32_t block_stride_b = 4u * NWAVES * kv_stride_b;
     auto issue_rows = [&](auto in_loop, const unsigned char* base, bool is_v, uint32_t full_off0, int tile, unsigned char* stage, int sk) {
@@ -454,11 +483,65 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             }
         }
     };
+    // Pages hold eight keys at least, so the four of a block are in one of them: its number is a scalar load (read-only memory:
+    // it counts against lgkmcnt, not against the tiles' vmcnt) and the block's address scalar arithmetic.  In the tile loop the
+    // numbers are loaded a step ahead; those of V(j) are the ones that K(j) took two steps before.
+    struct Pages {
+        uint32_t number[2];
+    };
+    auto look_up = [&](const Geo& of, int tile, int sk) {
+        typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+        const ConstInts row = (ConstInts)(uintptr_t)uniform(p.table + (int64_t)of.seq * p.table_len);
+        Pages n;
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            const int key = max(0, min(tile * kBN + 4 * (it * NWAVES + wave), sk - 1));
+            n.number[it] = (uint32_t)row[((int)of.kv_tok0 + key) >> p.log_page];
+        }
+        return n;
+    };
+    auto issue_paged = [&](auto in_loop, const __bf16* pool, const Geo& of, const Pages& pages, bool is_v, uint32_t full_off0, int tile,
+                           unsigned char* stage, int sk) {
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)stage + wave * 1024;
+        const unsigned char* const head = reinterpret_cast<const unsigned char*>(pool) + (uint64_t)(uint32_t)of.kvh * p.head_b;
+        auto base_of = [&](int it, int key) {
+            const int slot = ((int)of.kv_tok0 + key) & ((1 << p.log_page) - 1);
+            return head + min(pages.number[it], p.last_page) * p.page_b + (uint32_t)slot * p.row_b;
+        };
+        if (tile * kBN + kBN <= sk) {
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+                dma16<decltype(in_loop)::value>(base_of(it, tile * kBN + 4 * (it * NWAVES + wave)), full_off0, lds0 + it * NWAVES * 1024);
+        } else {
+            int ln;
+            asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(ln));
+            const int r_row = ln >> 4, r_pos = ln & 15, last = sk - 1;
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int key = 4 * (it * NWAVES + wave) + r_row;
+                const uint32_t col = is_v ? (uint32_t)((((r_pos >> 2) ^ (key & 3)) << 2) | (r_pos & 3)) * 16u
+                                          : (uint32_t)(r_pos ^ (key & 15)) * 16u;
+                const int from = min(tile * kBN + 4 * (it * NWAVES + wave), last & ~3);      // four keys of one page
+                dma16<false>(base_of(it, from), (uint32_t)(min(tile * kBN + key, last) - from) * kv_stride_b + col, lds0 + it * NWAVES * 1024);
+            }
+        }
+    };
+    Pages k_pages{}, ahead_pages{}, v_pages{};      // of K(j + 2), K(j + 1) and K(j)
     auto issue_k = [&](auto in_loop, int tile, unsigned char* stage) {
-        if (tile < n_tiles) issue_rows(in_loop, kbase, false, ldk_off0, tile, stage, sk);
+        if constexpr (kPaged) {
+            if (tile < n_tiles) {
+                if constexpr (!decltype(in_loop)::value) k_pages = look_up(g, tile, sk);
+                issue_paged(in_loop, p.k, g, k_pages, false, ldk_off0, tile, stage, sk);
+            }
+        } else if (tile < n_tiles) issue_rows(in_loop, kbase, false, ldk_off0, tile, stage, sk);
     };
     auto issue_v = [&](auto in_loop, int tile, unsigned char* stage) {
-        if (tile < n_tiles) issue_rows(in_loop, vbase, true, ldv_off0, tile, stage, sk);
+        if constexpr (kPaged) {
+            if (tile < n_tiles) issue_paged(in_loop, p.v, g, v_pages, true, ldv_off0, tile, stage, sk);
+            v_pages = ahead_pages;
+            ahead_pages = k_pages;
+            k_pages = look_up(g, tile + 3, sk);
+        } else if (tile < n_tiles) issue_rows(in_loop, vbase, true, ldv_off0, tile, stage, sk);
     };
     // All calls but the resumable sweep take Q through LDS, a private 8 KiB per wavefront (registers that are filled while the last tile is
     // worked on cost 140 spill instructions there); rows past the end re-read the last valid one, nothing of theirs is stored
@@ -497,6 +580,11 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             w.len_k = __builtin_amdgcn_readfirstlane(lo[3]);
             w.qtile = __builtin_amdgcn_readfirstlane(hi[0]);
             w.slot = __builtin_amdgcn_readfirstlane(hi[1]);
+            if constexpr (kPaged) {
+                const u32x2 range = *(const __attribute__((address_space(3))) u32x2*)(slot + 56);
+                w.pad[0] = __builtin_amdgcn_readfirstlane(range[0]);
+                w.pad[1] = __builtin_amdgcn_readfirstlane(range[1]);
+            }
             next = list_geometry(unit, w);
         } else {
             const int unit = round0 + n_slots < per_xcd ? dense_unit(round0 + n_slots) : -1;
@@ -505,6 +593,12 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             next = dense_geometry(unit);
         }
         const int n = tiles_of(next);
+        if constexpr (kPaged) {
+            if (n > 0) issue_paged(std::false_type{}, p.k, next, look_up(next, 0, next.sk), false, ldk_off0, 0, lds_k0, next.sk);
+            if (n > 1) issue_paged(std::false_type{}, p.k, next, look_up(next, 1, next.sk), false, ldk_off0, 1, lds_k1, next.sk);
+            issue_q(next);
+            return;
+        }
         const unsigned char* const kb = settled(kv_base(p.k, next));
         if (n > 0) issue_rows(std::true_type{}, kb, false, ldk_off0, 0, lds_k0, next.sk);
         if (n > 1) issue_rows(std::true_type{}, kb, false, ldk_off0, 1, lds_k1, next.sk);
@@ -769,6 +863,11 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             if (kList && wave == 0) take_next(count_up(share), par);
             end_of_iteration();
         }
+        if constexpr (kPaged) {       // (an item without keys looks at the row's first page number; the host sees to it that there is one)
+            v_pages = look_up(g, 0, sk);
+            ahead_pages = look_up(g, 1, sk);
+            k_pages = look_up(g, 2, sk);
+        }
         const u32x4 z = {0u, 0u, 0u, 0u};
         u32x4* const v1 = reinterpret_cast<u32x4*>(lds_v1 + wave * 2048 + lane * 16);
         v1[0] = z;
@@ -898,6 +997,18 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
         q_stride = kHeadDim;
         o_off0 = lse_off0 * kHeadDim;
     }
+    // A value that some rows do not see reaches them as 0 x value, which an infinite or NaN one is not: rows that come out so are
+    // looked at again behind the stores.
+    uint64_t odd_rows = 0;
+    if constexpr (kPaged) {
+        float odd = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) odd = fmaf(o[dt][r], 0.f, odd);
+        odd_rows = __ballot(causal && rw0 + l32 < sq && odd != odd);
+        odd_rows = (odd_rows | odd_rows >> 32) & 0xffffffffu;
+    }
     {
         const int row = rw0 + l32;
         const float l_tot = l_run + __shfl_xor(l_run, 32);
@@ -905,7 +1016,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
             const bool raw = kStops && stopped;   // a stopped item keeps its state as it stands
             const float inv = raw ? 1.f : (l_tot > 0.f ? 1.f / l_tot : 0.f);
             // (a piece whose weights are NaN says so in its LSE: span_merge_kernel tells it from one without a key)
-            const float none = kSpan && !whole && l_tot != l_tot ? l_tot : -INFINITY;
+            const float none = (kPaged || (kSpan && !whole)) && l_tot != l_tot ? l_tot : -INFINITY;
             const float lse = raw ? m_run : (l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2 : none);
             if (raw) p.l_part[(lse_off0 + row) * 2 + hl] = l_run;
             if (hl == 0) lse_ptr[lse_off0 + row] = lse;
@@ -945,6 +1056,36 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
                         }
                     }
                 }
+        }
+    }
+    if constexpr (kPaged) {
+        if (odd_rows != 0) {
+            // Only if a key that the wavefront's first row does not see has such a value (else they are what they are): the
+            // rows are worked out again, plainly.  As slow as it is rare: at most the rows of the tiles that hold such a key.
+            const PagedKv cache{reinterpret_cast<unsigned char*>(const_cast<__bf16*>(p.k)), reinterpret_cast<unsigned char*>(const_cast<__bf16*>(p.v)),
+                                p.page_b, p.row_b, p.head_b, p.last_page, p.log_page};
+            const int32_t* const table_row = p.table + (int64_t)g.seq * p.table_len;
+            const int first = (int)g.kv_tok0, lo = max(0, rw0 + delta + 1), hi = min(sk, max(0, wave_last + delta + kBN) / kBN * kBN);
+            bool found = false;
+            for (int key = lo + (lane >> 4); key < hi; key += 4) {
+                const int at = first + key;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(
+                    cache.v + page_in_cache(cache, table_row[at >> cache.log_page]) * cache.page_b +
+                    (at & ((1 << cache.log_page) - 1)) * (int64_t)cache.row_b + (int64_t)g.kvh * cache.head_b + 16 * (lane & 15));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) found |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+            }
+            if (!__any(found)) odd_rows = 0;
+            __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt 0: the rows' first results are in place
+            for (; odd_rows != 0; odd_rows &= odd_rows - 1) {
+                const int row = rw0 + __builtin_ctzll(odd_rows);
+                const __bf16* const qv = p.q + g.q_off0 + row * g.q_stride + 2 * lane;
+                const PlainRow fixed = plain_row(cache, table_row, g.kvh, (float)qv[0], (float)qv[1], p.scale_log2 * kLn2, first,
+                                                 first + max(0, min(sk, row + delta + 1)));
+                const int64_t idx = o_off0 + row * q_stride + 2 * lane;
+                if (out_f32) *reinterpret_cast<f32x2*>(reinterpret_cast<float*>(out_ptr) + idx) = f32x2{fixed.o0, fixed.o1};
+                else *reinterpret_cast<bf16x2*>(reinterpret_cast<__bf16*>(out_ptr) + idx) = __builtin_convertvector(f32x2{fixed.o0, fixed.o1}, bf16x2);
+            }
         }
     }
     if (kSweep && threadIdx.x == 0) {

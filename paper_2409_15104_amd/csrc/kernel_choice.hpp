@@ -324,6 +324,22 @@ inline int64_t decode_default_ranges(int cu, int n_q_heads, int n_kv_heads, int6
     return std::max<int64_t>(1, std::min<int64_t>(per_cu, sk / 1024));
 }
 
+// Which kernels a paged call runs on: paged_step_kernel (32 nt rows a unit) for sequences with few rows per KV head, the
+// pipelined kernel's work list for the others.  len_q: new tokens of a sequence at most, as far as the host knows.
+constexpr int kPagedFewRows = 64;
+struct PagedCut {
+    bool steps, list;
+    int nt, few_rows;        // few_rows: rows up to which a sequence goes to the steps where both run
+};
+inline PagedCut paged_cut(int64_t len_q, int64_t batch, int group) {
+    PagedCut c{};
+    c.list = len_q * group > kPagedFewRows;
+    c.few_rows = group <= 32 ? 32 : group <= 64 ? 64 : 0;
+    c.steps = !c.list || (batch > 1 && c.few_rows > 0);
+    c.nt = c.list ? c.few_rows / 32 : len_q * group <= 32 ? 1 : 2;
+    return c;
+}
+
 // Wavefronts per token of norm_rope_kernel, each with an equal part of the token's `rows` head rows, four of them at a time.
 inline int norm_rope_parts(int cu, int64_t tokens, int rows) {
     const int64_t quads = (rows + 3) / 4, wanted = ((int64_t)cu * 16 + tokens - 1) / std::max<int64_t>(1, tokens);

@@ -8,7 +8,7 @@ namespace {
 int64_t token_stride(int64_t stride, int heads) {
     const int64_t packed = (int64_t)heads * kHeadDim;
     if (stride == 0) return packed;
-    return stride >= packed && stride % 8 == 0 && stride <= ((int64_t)1 << 40) ? stride : -1;
+    return stride >= packed && stride % 8 == 0 && stride <= ((int64_t)1 << 25) ? stride : -1;
 }
 
 int check_cache(const pec_shape_t* s, const pec_paged_cache_t* c, PagedKv* out) {
@@ -51,18 +51,30 @@ int check_batch(const pec_paged_batch_t* b, int page_size, PagedBatch* out) {
     return PEC_OK;
 }
 
-// Workspace of pec_attn_paged: the pieces' O and LSE, two slots for each span of either variant of paged_step_kernel, and the
-// steps ahead of every sequence.
+// Workspace of pec_attn_paged.  Partial results (O and LSE of so many rows) of paged_step_kernel's spans, two slots each, or of
+// fwd_il_kernel's items, 256 rows each -- the two run one after the other; the steps ahead of every sequence; the work list.
 struct PagedLayout {
-    size_t off_lse, off_prefix, bytes;
+    int log_heads, bm, units;            // of a work list's items
+    int64_t capacity, slots;
+    size_t off_lse, off_prefix, off_work, off_counters, off_splits, bytes;
 };
-PagedLayout paged_layout(int cu, int32_t batch) {
+constexpr int64_t kPagedSlabs = 1024;    // items' partial results: four for every compute unit
+PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_t total_q) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-    const size_t slot_rows = (size_t)cu * kPagedWaves1 * 2 * 32;
     PagedLayout l;
-    l.off_lse = slot_rows * kHeadDim * sizeof(float);
-    l.off_prefix = up(l.off_lse + slot_rows * sizeof(float));
-    l.bytes = up(l.off_prefix + ((size_t)batch + 1) * sizeof(int32_t));
+    l.log_heads = most_log_heads_per_item(shape->n_q_heads, shape->n_kv_heads);
+    l.bm = kBM >> l.log_heads;
+    l.units = shape->n_q_heads >> l.log_heads;
+    const bool list = total_q * (shape->n_q_heads / shape->n_kv_heads) > kPagedFewRows;
+    l.slots = list ? kPagedSlabs / l.units : 0;
+    l.capacity = list ? total_q / l.bm + batch + l.slots : 0;
+    const size_t rows = std::max((size_t)cu * kPagedWaves1 * 2 * 32, (size_t)l.slots * l.units * kBM);
+    l.off_lse = rows * kHeadDim * sizeof(float);
+    l.off_prefix = up(l.off_lse + rows * sizeof(float));
+    l.off_work = up(l.off_prefix + ((size_t)batch + 1) * sizeof(int32_t));
+    l.off_counters = up(l.off_work + (size_t)l.capacity * sizeof(WorkItem));
+    l.off_splits = l.off_counters + 256;
+    l.bytes = up(l.off_splits + (size_t)(l.slots / 2 + 1) * sizeof(PagedSplit));
     return l;
 }
 
@@ -172,7 +184,8 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
 
 size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q) {
     if (!shape || shape->n_q_heads <= 0 || shape->n_kv_heads <= 0 || batch < 0 || total_q < 0) return 0;
-    return paged_layout(compute_units(), batch).bytes;
+    if (shape->n_q_heads % shape->n_kv_heads != 0) return 0;
+    return paged_layout(compute_units(), shape, batch, total_q).bytes;
 }
 
 int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,
@@ -207,31 +220,88 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
     }
     if (batch->batch > kPagedChunks * 64) return PEC_ERR_UNSUPPORTED;
-    const int cu = std::max(8, compute_units() & ~7);
+    const int cu = std::max(8, compute_units() & ~7), g = p.group;
     const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
-    const int nt = len_q * p.group <= 32 ? 1 : 2;
-    // every tile step has a number
-    const int64_t row_tiles = batch->total_q * p.group / (32 * nt) + batch->batch;
-    if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) * p.n_kv_heads > 2147483647.0) return PEC_ERR_UNSUPPORTED;
-    const PagedLayout l = paged_layout(compute_units(), batch->batch);
+    const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
     char* const ws = static_cast<char*>(workspace);
-    PagedStepParams s{};
-    s.a = p;
-    s.part_out = reinterpret_cast<float*>(ws);
-    s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
-    s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-    s.min_span = 2;
-    s.most_rows = 0x7fffffff;
-    s.n_spans = cu * (nt == 1 ? kPagedWaves1 : kPagedWaves2);
-    if (nt == 1)
-        hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
-    else
-        hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
+    const PagedCut cut = paged_cut(len_q, batch->batch, g);
+
+    if (cut.steps) {
+        PagedStepParams s{};
+        s.a = p;
+        s.part_out = reinterpret_cast<float*>(ws);
+        s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+        s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
+        s.min_span = 2;
+        s.most_rows = cut.list ? cut.few_rows : 0x7fffffff;
+        s.n_spans = cu * (cut.nt == 1 ? kPagedWaves1 : kPagedWaves2);
+        // every tile step has a number
+        const int64_t per_seq = (std::min<int64_t>(cut.list ? cut.few_rows : len_q * g, len_q * g) + 32 * cut.nt - 1) / (32 * cut.nt);
+        const int64_t row_tiles = cut.list ? batch->batch * per_seq : batch->total_q * g / (32 * cut.nt) + batch->batch;
+        if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) * p.n_kv_heads > 2147483647.0) return PEC_ERR_UNSUPPORTED;
+        if (cut.nt == 1)
+            hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
+        else
+            hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
+        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+        const dim3 grid((unsigned)std::min(batch->batch, 4096), (unsigned)shape->n_q_heads, (unsigned)std::min<int64_t>(16, std::max<int64_t>(1, per_seq)));
+        hipLaunchKernelGGL(paged_merge_kernel, grid, dim3(kPagedMergeThreads), 0, st, s, 32 * cut.nt);
+        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    }
+    if (!cut.list) return PEC_OK;
+    if (l.capacity * l.units > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
+    PagedListParams w{};
+    w.batch = p.batch;
+    w.bm = l.bm;
+    w.group = g;
+    w.units = l.units;
+    w.causal = p.causal;
+    w.few_rows = cut.steps ? cut.few_rows : 0;
+    w.capacity = (int32_t)l.capacity;
+    w.slot_capacity = (int32_t)l.slots;
+    w.cu = cu;
+    w.work = reinterpret_cast<WorkItem*>(ws + l.off_work);
+    w.counters = reinterpret_cast<int32_t*>(ws + l.off_counters);
+    w.splits = reinterpret_cast<PagedSplit*>(ws + l.off_splits);
+    hipLaunchKernelGGL(paged_list_kernel, dim3(1), dim3(1024), 0, st, w);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-    const int64_t per_seq = std::min<int64_t>(16, (len_q * p.group + 32 * nt - 1) / (32 * nt));
-    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)std::min(batch->batch, 4096), (unsigned)shape->n_q_heads, (unsigned)per_seq),
-                       dim3(kPagedMergeThreads), 0, st, s, 32 * nt);
-    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    FwdParams f{};
+    f.q = p.q;
+    f.k = reinterpret_cast<const __bf16*>(p.cache.k);
+    f.v = reinterpret_cast<const __bf16*>(p.cache.v);
+    f.out = out;
+    f.lse = lse;
+    f.lse_stride = batch->total_q;
+    f.causal = p.causal;
+    f.n_q_heads = p.n_q_heads;
+    f.n_kv_heads = p.n_kv_heads;
+    f.group = g;
+    f.log_heads = l.log_heads;
+    f.n_items = (int32_t)l.capacity;
+    f.out_f32 = p.out_f32;
+    f.scale_log2 = p.scale_log2;
+    f.work = w.work;
+    f.n_work = w.counters;
+    f.sched = w.counters + 8;
+    f.q_row_stride = p.q_stride;
+    f.part_out = reinterpret_cast<float*>(ws);
+    f.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+    f.table = p.batch.table_len > 0 ? p.batch.table : p.batch.cu_q;      // (a word to look at where there is no page: no key is in it)
+    f.table_len = p.batch.table_len;
+    f.page_b = p.cache.page_b;
+    f.row_b = p.cache.row_b;
+    f.head_b = p.cache.head_b;
+    f.last_page = p.cache.last_page;
+    f.log_page = p.cache.log_page;
+    const int64_t groups = std::min<int64_t>(cu, (l.capacity * l.units + 7) / 8 * 8);
+    hipLaunchKernelGGL(fwd_il_kernel<kFwdPaged>, dim3((unsigned)groups), dim3(512), 0, st, f);
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    if (l.slots > 1) {
+        hipLaunchKernelGGL(paged_ranges_merge_kernel, dim3((unsigned)std::min<int64_t>(l.slots / 2, 64), (unsigned)l.units, 8), dim3(256), 0, st, w,
+                           f.part_out, f.part_lse, l.log_heads, p.n_q_heads, p.out_f32, out, lse);
+        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    }
+    return PEC_OK;
 }
 
 }  // extern "C"

@@ -44,6 +44,59 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& b, int i) {
 // Number of the page, inside the cache whatever the table says.
 __device__ __forceinline__ uint32_t page_in_cache(const PagedKv& c, int32_t number) { return min((uint32_t)number, c.last_page); }
 
+// O (two dims per lane) and LSE of one query row over keys [key0, key_end) of its sequence, written out plainly: fp32 weights, the
+// exact running maximum, no key looked at that the row does not see.  In blocks of 64 keys: a lane per key for the scores, then
+// two dims per lane for O += p V, the weights handed round.  q0, q1: the row's values 2 * lane and 2 * lane + 1.
+struct PlainRow {
+    float o0, o1, lse;
+};
+__device__ __forceinline__ PlainRow plain_row(const PagedKv& cache, const int32_t* table_row, int kvh, float q0, float q1,
+                                              float scale, int key0, int key_end) {
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    const int64_t head_off = (int64_t)kvh * cache.head_b;
+    auto row_of = [&](int key) {
+        return page_in_cache(cache, table_row[key >> cache.log_page]) * cache.page_b +
+               (key & ((1 << cache.log_page) - 1)) * (int64_t)cache.row_b + head_off;
+    };
+    auto of_lane = [](float x, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l)); };
+    float m = -INFINITY, den = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int k0 = key0; k0 < key_end; k0 += 64) {
+        const int n = min(64, key_end - k0);
+        const u32x4* const row = reinterpret_cast<const u32x4*>(cache.k + row_of(k0 + min(lane, n - 1)));
+        float dot = 0.f;
+        for (int c = 0; c < 16; ++c) {
+            const u32x4 x = row[c];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                dot = fmaf(__builtin_bit_cast(float, x[e] << 16), of_lane(q0, 4 * c + e), dot);
+                dot = fmaf(__builtin_bit_cast(float, x[e] & 0xffff0000u), of_lane(q1, 4 * c + e), dot);
+            }
+        }
+        const float s = lane < n ? dot * scale : -INFINITY;
+        float top = s;       // NaN is passed over here and comes back in with the weights
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        const float m_new = fmaxf(m, top);
+        const float ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = expf(m - ref);
+        const float p = lane < n ? expf(s - ref) : 0.f;
+        float sum = p;
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+        den = den * alpha + sum;
+        o0 *= alpha;
+        o1 *= alpha;
+        for (int j = 0; j < n; ++j) {
+            const float w = of_lane(p, j);
+            const uint32_t x = reinterpret_cast<const uint32_t*>(cache.v + row_of(k0 + j))[lane];
+            o0 = fmaf(w, __builtin_bit_cast(float, x << 16), o0);
+            o1 = fmaf(w, __builtin_bit_cast(float, x & 0xffff0000u), o1);
+        }
+        m = m_new;
+    }
+    if (key_end <= key0) return PlainRow{0.f, 0.f, -INFINITY};
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    return PlainRow{o0 * inv, o1 * inv, den == 0.f ? -INFINITY : m + logf(den)};
+}
+
 // The sequence that owns packed row `token`, or -1.  Called by whole wavefronts with a uniform token: 64 offsets are looked at
 // at a time, so 4,096 sequences take two trips to memory and not the twelve of a binary search.
 __device__ __forceinline__ int paged_owner(const PagedBatch& b, int token) {

@@ -1,0 +1,229 @@
+// Work list of fwd_il_kernel<kFwdPaged>, built on the device from lengths that only the device knows, and the merge of the
+// items' partial results.
+//
+// An item is a query tile (bm positions of a sequence, for the 256 / bm heads that share a workgroup) and a range of its keys.
+// Few items would leave compute units idle, and so would a few more than a whole number per compute unit, so the keys are cut
+// into ranges where the estimate below says so; ranges of a sequence start at the same keys for all of its tiles, and the list
+// has them side by side, so that the workgroups of an XCD walk the same keys at the same time and find them in its L2.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "aux_kernels.hpp"
+#include "paged_common.hpp"
+
+namespace pec {
+
+struct PagedSplit {      // a query tile whose keys are cut into ranges
+    int32_t seq, qtile, slot0, n_ranges;
+};
+struct PagedListParams {
+    PagedBatch batch;
+    int32_t bm, group, units, causal;        // positions per item; units of an item, over all KV heads
+    int32_t few_rows;                        // sequences with at most so many rows per KV head are another launch's
+    int32_t capacity, slot_capacity, cu;
+    WorkItem* work;
+    int32_t* counters;                       // [0] items, [2] split tiles, [8 .. 15] draw counters
+    PagedSplit* splits;
+};
+
+constexpr int kPagedListSeqs = 1024, kPagedListBuckets = 1024;
+
+// Keys that tile t of the sequence walks, and the first of its tiles that walks more than x.
+struct PagedTiles {
+    int n, len_q, len_k, bm, causal;
+    __device__ __forceinline__ PagedTiles(const PagedSeq& s, const PagedListParams& p) : len_q(s.len_q), len_k(s.len_k), bm(p.bm), causal(p.causal) {
+        n = (int64_t)len_q * p.group > p.few_rows ? (len_q + bm - 1) / bm : 0;
+    }
+    __device__ __forceinline__ int keys(int t) const {
+        return causal ? max(0, len_k - len_q + (int)min((int64_t)len_q, (int64_t)(t + 1) * bm)) : len_k;
+    }
+    __device__ __forceinline__ int first_beyond(int x) const {
+        if (len_k <= x) return n;
+        const int y = x - (len_k - len_q);
+        return causal && y > 0 ? min(n - 1, y / bm) : 0;
+    }
+    // items of all tiles with ranges of `range` keys, and how many tiles are not cut
+    __device__ __forceinline__ int items(int range, int* uncut) const {
+        *uncut = first_beyond(range);
+        int sum = n;
+        for (int64_t x = range; x < len_k; x += range) sum += n - first_beyond((int)x);
+        return sum;
+    }
+};
+
+// Keys per range, as the smallest of sixteen estimates, one per wavefront; 0x40000000: no tile is cut.  In tile steps of 64
+// keys: an item takes 8 besides its own (its first loads, its results), its partial results 4 more, and their merge with its
+// launch 8 per call; items that are all alike run in whole rounds, others even out but for half an item at the end.
+__global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams p) {
+    struct Seq {
+        PagedSeq s;
+        int n_items;
+    };
+    __shared__ Seq seqs[kPagedListSeqs];
+    __shared__ int32_t bucket[kPagedListBuckets];
+    __shared__ int32_t red[16], n_slots, n_split, range_lds;
+    __shared__ float cost[16];
+    __shared__ int32_t cand[16];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const PagedBatch& bt = p.batch;
+    if (tid == 0) n_slots = n_split = 0;
+    if (tid >= 8 && tid < 16) p.counters[tid] = 0;
+
+    // ---- the longest walk, then the estimates
+    int longest = 0;
+    for (int b = tid; b < bt.batch; b += 1024) {
+        const PagedTiles t(paged_seq(bt, b), p);
+        if (t.n > 0) longest = max(longest, t.keys(t.n - 1));
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off));
+    if (lane == 0) red[wave] = longest;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) longest = max(longest, red[w]);
+    const int whole = (longest + kBN - 1) / kBN;           // tile steps of the longest item
+    {
+        // candidates: the longest walk in 1, 2, 3, ... 8, 10, 12, 16, 20, 24, 32, 48, 64 ranges of at least 16 steps
+        const int parts = wave < 8 ? wave + 1 : wave == 8 ? 10 : wave == 9 ? 12 : wave == 10 ? 16 : wave == 11 ? 20
+                        : wave == 12 ? 24 : wave == 13 ? 32 : wave == 14 ? 48 : 64;
+        const int steps = max(16, (whole + parts - 1) / parts), range = wave == 0 || p.slot_capacity == 0 ? 0x40000000 : steps * kBN;
+        int64_t all_keys = 0;
+        int items = 0, uncut = 0, tiles = 0;
+        for (int b = lane; b < bt.batch; b += 64) {
+            const PagedTiles t(paged_seq(bt, b), p);
+            if (t.n == 0) continue;
+            int u;
+            items += t.items(range, &u);
+            uncut += u;
+            tiles += t.n;
+            all_keys += ((int64_t)t.keys(0) + t.keys(t.n - 1)) * t.n / 2;
+        }
+        float keys = (float)all_keys;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            items += __shfl_xor(items, off);
+            uncut += __shfl_xor(uncut, off);
+            tiles += __shfl_xor(tiles, off);
+            keys += __shfl_xor(keys, off);
+        }
+        if (lane == 0) {
+            const int cut = items - uncut;      // items with partial results
+            const float units = (float)p.units, work = (keys / kBN + 0.5f * tiles + 8.f * items + 4.f * cut) * units / p.cu;
+            const float one = (float)min(whole, range / kBN) + 8.f + (cut > 0 ? 4.f : 0.f);
+            const float rounds = ceilf(items * units / p.cu);
+            float c = fmaxf(one, fminf(rounds * one, work + 0.5f * one)) + (cut > 0 ? 8.f : 0.f);
+            if (cut > p.slot_capacity) c = INFINITY;
+            cost[wave] = c;
+            cand[wave] = range;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int best = 0;
+        for (int i = 1; i < 16; ++i)
+            if (cost[i] < cost[best]) best = i;
+        range_lds = cand[best];
+    }
+    for (int t = tid; t < kPagedListBuckets; t += 1024) bucket[t] = 0;
+    __syncthreads();
+    const int range = range_lds;
+
+    // ---- sequences by their longest walk, the items of a sequence together: range by range, the last tile first
+    auto load_seq = [&](int c0) {
+        const int b = c0 + tid;
+        if (b >= bt.batch) return;
+        Seq q;
+        q.s = paged_seq(bt, b);
+        int u;
+        const PagedTiles t(q.s, p);
+        q.n_items = t.n > 0 ? t.items(range, &u) : 0;
+        seqs[tid] = q;
+    };
+    auto bucket_of = [&](const Seq& q) {
+        const PagedTiles t(q.s, p);
+        return t.n > 0 ? (int)min((int64_t)kPagedListBuckets - 1, (int64_t)t.keys(t.n - 1) * kPagedListBuckets / (longest + 1)) : 0;
+    };
+    for (int c0 = 0; c0 < bt.batch; c0 += kPagedListSeqs) {
+        if (c0 > 0) __syncthreads();
+        load_seq(c0);
+        if (c0 + tid < bt.batch && seqs[tid].n_items > 0) atomicAdd(&bucket[bucket_of(seqs[tid])], seqs[tid].n_items);
+    }
+    __syncthreads();
+    const int total = block_suffix_sum_1024(bucket, kPagedListBuckets, red);
+    if (tid == 0) p.counters[0] = min(total, p.capacity);
+    for (int c0 = 0; c0 < bt.batch; c0 += kPagedListSeqs) {
+        if (bt.batch > kPagedListSeqs) {
+            __syncthreads();
+            load_seq(c0);
+        }
+        __shared__ int32_t pos0[kPagedListSeqs];
+        if (c0 + tid < bt.batch && seqs[tid].n_items > 0) pos0[tid] = atomicAdd(&bucket[bucket_of(seqs[tid])], seqs[tid].n_items);
+        __syncthreads();
+        const int n = min(bt.batch - c0, kPagedListSeqs);
+        for (int i = wave; i < n; i += 16) {
+            const Seq q = seqs[i];
+            if (q.n_items == 0) continue;
+            const PagedTiles t(q.s, p);
+            for (int tile = lane; tile < t.n; tile += 64) {
+                const int keys = t.keys(tile), n_ranges = max(1, (int)(((int64_t)keys + range - 1) / range));
+                int slot0 = -1;
+                if (n_ranges > 1) {
+                    slot0 = atomicAdd(&n_slots, n_ranges);
+                    if (slot0 + n_ranges > p.slot_capacity) continue;      // (never, unless the offsets change under the launch)
+                    p.splits[atomicAdd(&n_split, 1)] = PagedSplit{c0 + i, tile, slot0, n_ranges};
+                }
+                int pos = pos0[i] + t.n - 1 - tile;
+                for (int r = 0; r < n_ranges; ++r) {
+                    if (r > 0) pos += t.n - (r == 1 ? 0 : t.first_beyond((r - 1) * range));
+                    const int key0 = r * range;
+                    if ((uint32_t)pos < (uint32_t)p.capacity)
+                        p.work[pos] = WorkItem{q.s.q0, q.s.len_q, c0 + i, q.s.len_k, tile, slot0 < 0 ? -1 : slot0 + r,
+                                               {n_ranges > 1 ? key0 : 0, n_ranges > 1 ? min(keys, key0 + range) : keys}};
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0) p.counters[2] = n_split;
+}
+
+// Merges the ranges of split tiles, 32 rows (those of a wavefront of fwd_il_kernel) per workgroup: grid (split tiles at most,
+// units of an item, 8).
+__global__ __launch_bounds__(256) void paged_ranges_merge_kernel(const PagedListParams p, const float* part_out, const float* part_lse,
+                                                                 int log_heads, int n_q_heads, int out_f32, void* out, float* lse) {
+    const int n_split = p.counters[2], unit = blockIdx.y, strip = blockIdx.z;
+    const int per_kvh = p.group >> log_heads, kvh = unit / per_kvh, u = unit % per_kvh;
+    const int head = kvh * p.group + (u << log_heads) + (strip >> (3 - log_heads)), c = threadIdx.x & 31;
+    for (int i = blockIdx.x; i < n_split; i += gridDim.x) {
+        const PagedSplit sp = p.splits[i];
+        const PagedSeq s = paged_seq(p.batch, sp.seq);
+        const int pos0 = sp.qtile * p.bm + ((strip << 5) & (p.bm - 1));
+        for (int r = threadIdx.x >> 5; r < 32; r += 8) {
+            if (pos0 + r >= s.len_q) break;
+            auto row_of = [&](int n) { return ((int64_t)(sp.slot0 + n) * p.units + unit) * 256 + strip * 32 + r; };
+            float mx = -INFINITY, den = 0.f;
+            for (int n = 0; n < sp.n_ranges; ++n) mx = fmaxf(mx, part_lse[row_of(n)]);      // (NaN: as if it were not there)
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int n = 0; n < sp.n_ranges; ++n) {
+                const int64_t at = row_of(n);
+                const float w = expf(part_lse[at] - ref);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(part_out + at * kHeadDim + 4 * c);
+                den += w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = fmaf(w, x[e], a[e]);
+            }
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] *= inv;
+            const int64_t token = s.q0 + pos0 + r, idx = (token * n_q_heads + head) * kHeadDim + 4 * c;
+            if (out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + idx) = a;
+            else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + idx) = __builtin_convertvector(a, bf16x4);
+            if (c == 0) lse[(int64_t)head * p.batch.total_q + token] = den == 0.f ? -INFINITY : ref + logf(den);
+        }
+    }
+}
+
+}  // namespace pec

@@ -23,6 +23,7 @@
 #include "fwd_split_kernel.hpp"
 #include "kernel_choice.hpp"
 #include "norm_rope_kernel.hpp"
+#include "paged_list.hpp"
 #include "paged_simple_kernel.hpp"
 #include "paged_step_kernel.hpp"
 #include "probes.hpp"
