@@ -232,20 +232,27 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         s.part_out = reinterpret_cast<float*>(ws);
         s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
         s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-        s.min_span = 2;
         s.most_rows = cut.list ? cut.few_rows : 0x7fffffff;
-        s.n_spans = cu * (cut.nt == 1 ? kPagedWaves1 : kPagedWaves2);
+        const int waves = cu * (cut.nt == 1 ? kPagedWaves1 : kPagedWaves2);
+        if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
+        s.n_spans = waves / p.n_kv_heads;
         // every tile step has a number
         const int64_t per_seq = (std::min<int64_t>(cut.list ? cut.few_rows : len_q * g, len_q * g) + 32 * cut.nt - 1) / (32 * cut.nt);
         const int64_t row_tiles = cut.list ? batch->batch * per_seq : batch->total_q * g / (32 * cut.nt) + batch->batch;
-        if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) * p.n_kv_heads > 2147483647.0) return PEC_ERR_UNSUPPORTED;
+        if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;
         if (cut.nt == 1)
             hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
         else
             hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-        const dim3 grid((unsigned)std::min(batch->batch, 4096), (unsigned)shape->n_q_heads, (unsigned)std::min<int64_t>(16, std::max<int64_t>(1, per_seq)));
-        hipLaunchKernelGGL(paged_merge_kernel, grid, dim3(kPagedMergeThreads), 0, st, s, 32 * cut.nt);
+        const int tokens = (int)std::max<int64_t>(1, std::min(len_q, (int64_t)(cut.nt * 32 / g)));
+        const int64_t rows = (int64_t)batch->batch * tokens;
+        if (rows * shape->n_q_heads >= (int64_t)cu * 8)      // rows for every wavefront
+            hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), (unsigned)shape->n_q_heads),
+                               dim3(kPagedMergeThreads), 0, st, s, 32 * cut.nt, tokens);
+        else
+            hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, (unsigned)shape->n_q_heads), dim3(kPagedMergeThreads), 0, st, s,
+                               32 * cut.nt, tokens);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     }
     if (!cut.list) return PEC_OK;
