@@ -340,9 +340,9 @@ inline PagedCut paged_cut(int64_t len_q, int64_t batch, int group) {
     return c;
 }
 
-// Wavefronts per token of norm_rope_kernel, each with an equal part of the token's `rows` head rows, four of them at a time.
-inline int norm_rope_parts(int cu, int64_t tokens, int rows) {
-    const int64_t quads = (rows + 3) / 4, wanted = ((int64_t)cu * 16 + tokens - 1) / std::max<int64_t>(1, tokens);
+// Wavefronts per token of norm_rope_kernel, each with an equal part of the token's groups of four head rows.
+inline int norm_rope_parts(int cu, int64_t tokens, int64_t quads) {
+    const int64_t wanted = ((int64_t)cu * 16 + tokens - 1) / std::max<int64_t>(1, tokens);
     return (int)std::max<int64_t>(1, std::min(quads, wanted));
 }
 

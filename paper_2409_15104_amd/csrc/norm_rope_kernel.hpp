@@ -3,10 +3,15 @@
 //   x' = x w / sqrt(mean(x^2) + eps)                      over the 128 dims of a head row, if there is a weight
 //   (a, b) -> (a cos - b sin, b cos + a sin)              of the pairs (i, i + R / 2) or (2 i, 2 i + 1) of the first R dims
 //
-// all in fp32, rounded to bf16 once at the end.  Memory-bound: a head row is 256 bytes in and 256 out for 128 x 7 flop, so it is
-// read once, by 16 lanes with 16 bytes each, and everything is done in registers: the sum of squares by four row rotations
-// (DPP), the pairs of the usual R = 128 by one more.  A wavefront keeps to one token and takes four head rows at a time:
-// the token's angles are fetched once for all of them, and its place in the cache looked up once.
+// all in fp32, rounded to bf16 once at the end.  Memory-bound: a head row is 256 bytes in and 256 out, so it is read once, by 16
+// lanes with 16 bytes each, and everything is done in registers: the sum of squares by four row rotations (DPP), the pairs of
+// the usual R = 128 by one more.  A wavefront keeps to one token and takes four head rows at a time: the token's angles are
+// fetched once for all of them, and its place in the cache looked up once.
+//
+// The vector ALU comes close behind memory (a wavefront instruction for every 1 KiB holds up its SIMD for 4 cycles, and 6 TB/s
+// are 1 KiB per compute unit every 100), so the norm's factor, which all of a row shares, is applied last, and the weights go into
+// the token's angles: y = (x (w cos) + partner(x) (partner(w) sin)) / |x|, 24 operations per 8 values, and 1 / sqrt is one
+// instruction (v_rsq_f32, 1 ulp).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -32,8 +37,6 @@ struct NormRopeParams {
 };
 
 constexpr int kNormRopeThreads = 256;
-constexpr int kNormRopeAhead = 4;            // groups of four head rows requested together
-
 __device__ __forceinline__ float row_rotated(float x, int ctrl) {     // 16 lanes rotated among themselves; ctrl is a constant
     switch (ctrl) {
         case 1: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x121, 0xf, 0xf, true));
@@ -53,28 +56,25 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
     const int64_t w = (int64_t)blockIdx.x * (kNormRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int token = (int)(w / p.parts), part = (int)(w % p.parts);
     if (token >= p.tokens) return;
-    const int rows = p.n_q_heads + (APPEND ? 2 : 1) * p.n_kv_heads;
-    const int quads = (rows + 3) / 4, per_part = (quads + p.parts - 1) / p.parts;
-    const int quad_end = min(quads, (part + 1) * per_part);
-
-    // where head row r of the token comes from (null: there is no such row)
-    auto source = [&](int r) -> const __bf16* {
-        if (r < p.n_q_heads) return p.q + token * p.q_stride + r * kHeadDim;
-        r -= p.n_q_heads;
-        if (r < p.n_kv_heads) return p.k + token * p.k_stride + r * kHeadDim;
-        r -= p.n_kv_heads;
-        if (APPEND && r < p.n_kv_heads) return p.v + token * p.v_stride + r * kHeadDim;
-        return nullptr;
-    };
-    auto fetch = [&](int quad) {
-        const __bf16* src = quad < quad_end ? source(4 * quad + sub) : nullptr;
+    // groups of four head rows: queries, keys, values
+    const int q_quads = (p.n_q_heads + 3) / 4, k_quads = (p.n_kv_heads + 3) / 4, quads = q_quads + (APPEND ? 2 : 1) * k_quads;
+    const int per_part = (quads + p.parts - 1) / p.parts, begin = part * per_part, end = min(quads, begin + per_part);
+    // Groups requested ahead.  With a cache one: the lookups are a chain of three trips, which more wavefronts (fewer registers)
+    // hide better; 5,300 tokens of 32 / 8 heads 37.2 us with two, 31.7 with one, without a cache 16,384 of 64 / 8 122 and 124.
+    constexpr int kNormRopeAhead = APPEND ? 1 : 2;
+    enum { Q, K, V };
+    auto kind_of = [&](int i) { return i < q_quads ? Q : i < q_quads + k_quads ? K : V; };
+    auto fetch = [&](int i) {
         u32x4 x = {0u, 0u, 0u, 0u};
-        if (src) x = *reinterpret_cast<const u32x4*>(src + 8 * c);
+        if (i >= end) return x;
+        const int kind = kind_of(i), head = 4 * (i - (kind == Q ? 0 : kind == K ? q_quads : q_quads + k_quads)) + sub;
+        const __bf16* const row = kind == Q ? p.q + token * p.q_stride : kind == K ? p.k + token * p.k_stride : p.v + token * p.v_stride;
+        if (head < (kind == Q ? p.n_q_heads : p.n_kv_heads)) x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + head * kHeadDim + 8 * c));
         return x;
     };
     u32x4 ahead[kNormRopeAhead];
 #pragma unroll
-    for (int i = 0; i < kNormRopeAhead; ++i) ahead[i] = fetch(part * per_part + i);
+    for (int i = 0; i < kNormRopeAhead; ++i) ahead[i] = fetch(begin + i);
 
     // ---- the token's position, and its place in the cache
     int64_t at;
@@ -98,11 +98,17 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
 
     // ---- angles: y[i] = x[i] cs[i] + partner(x)[i] sn[i], the signs in sn
     float cs[8], sn[8];
-    int partner = lane;
+    int partner = lane, partner_dim = 8 * c;         // of the lane's first value (kPairsNext: the pairs sit inside a lane)
+    const bool turns = PAIRS != kPairsNone && 8 * c < p.rotary;
     if constexpr (PAIRS != kPairsNone) {
         const int half = p.rotary >> 1;
         const float* row = p.table + max((int64_t)0, min(at, (int64_t)p.n_positions - 1)) * p.rotary;
-        if (8 * c < p.rotary) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            cs[i] = 1.f;
+            sn[i] = 0.f;
+        }
+        if (turns) {
             if constexpr (PAIRS == kPairsNext) {
                 const f32x4 co = *reinterpret_cast<const f32x4*>(row + 4 * c), si = *reinterpret_cast<const f32x4*>(row + half + 4 * c);
 #pragma unroll
@@ -114,6 +120,7 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                 const bool upper = 8 * c >= half;
                 const float* col = row + 8 * c - (upper ? half : 0);
                 partner = upper ? lane - half / 8 : lane + half / 8;
+                partner_dim += upper ? -half : half;
 #pragma unroll
                 for (int i = 0; i < 8; i += 4) {
                     const f32x4 co = *reinterpret_cast<const f32x4*>(col + i), si = *reinterpret_cast<const f32x4*>(col + half + i);
@@ -124,44 +131,48 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                     }
                 }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                cs[i] = 1.f;
-                sn[i] = 0.f;
-            }
-        }
-    }
-    float qw[8], kw[8];
-    if constexpr (NORM) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            qw[i] = p.q_weight ? p.q_weight[8 * c + i] : 1.f;
-            kw[i] = p.k_weight ? p.k_weight[8 * c + i] : 1.f;
         }
     }
 
-    // ---- head rows, four at a time
-    for (int quad0 = part * per_part; quad0 < quad_end; quad0 += kNormRopeAhead) {
-        u32x4 now[kNormRopeAhead];
+    // ---- head rows, four at a time; the weights of their kind go into the angles
+    float a[8], b[8];
+    bool normed = false;
+    int kind_now = -1;
+    for (int i0 = begin; i0 < end; i0 += kNormRopeAhead) {
 #pragma unroll
-        for (int i = 0; i < kNormRopeAhead; ++i) {
-            now[i] = ahead[i];
-            ahead[i] = fetch(quad0 + kNormRopeAhead + i);
-        }
+        for (int j = 0; j < kNormRopeAhead; ++j) {
+            const int i = i0 + j;
+            if (i >= end) break;
+            const u32x4 raw = ahead[j];
+            ahead[j] = fetch(i + kNormRopeAhead);
+            const int kind = kind_of(i), head = 4 * (i - (kind == Q ? 0 : kind == K ? q_quads : q_quads + k_quads)) + sub;
+            u32x4 y = raw;
+            if ((NORM || PAIRS != kPairsNone) && kind != V) {
+                if (kind != kind_now) {
+                    kind_now = kind;
+                    const float* const weight = kind == Q ? p.q_weight : p.k_weight;
+                    normed = NORM && weight != nullptr;
 #pragma unroll
-        for (int i = 0; i < kNormRopeAhead; ++i) {
-            const int r = 4 * (quad0 + i) + sub;
-            const bool is_q = r < p.n_q_heads, is_k = !is_q && r < p.n_q_heads + p.n_kv_heads;
-            u32x4 y = now[i];
-            if constexpr (NORM || PAIRS != kPairsNone) {
+                    for (int e = 0; e < 8; ++e) {
+                        a[e] = PAIRS == kPairsNone ? 1.f : cs[e];
+                        b[e] = PAIRS == kPairsNone ? 0.f : sn[e];
+                    }
+                    if (NORM && normed) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            a[e] *= weight[8 * c + e];
+                            if (PAIRS != kPairsNone) b[e] *= weight[PAIRS == kPairsNext ? 8 * c + (e ^ 1) : partner_dim + e];
+                        }
+                    }
+                }
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    x[2 * e] = __builtin_bit_cast(float, now[i][e] << 16);
-                    x[2 * e + 1] = __builtin_bit_cast(float, now[i][e] & 0xffff0000u);
+                    x[2 * e] = __builtin_bit_cast(float, raw[e] << 16);
+                    x[2 * e + 1] = __builtin_bit_cast(float, raw[e] & 0xffff0000u);
                 }
-                if constexpr (NORM) {
+                float inv = 1.f;
+                if (NORM && normed) {
                     float ss = 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
@@ -169,42 +180,31 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                     ss += row_rotated(ss, 4);
                     ss += row_rotated(ss, 2);
                     ss += row_rotated(ss, 1);
-                    const bool has = is_q ? p.q_weight != nullptr : p.k_weight != nullptr;
-                    const float inv = has ? 1.f / sqrtf(fmaf(ss, 1.f / kHeadDim, p.eps)) : 1.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * (is_q ? qw[e] : kw[e]);
+                    inv = __builtin_amdgcn_rsqf(fmaf(ss, 1.f / kHeadDim, p.eps));
                 }
                 float z[8];
-                if constexpr (PAIRS == kPairsNone) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = x[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < 8; ++e) {
+                    z[e] = x[e] * a[e];
+                    if constexpr (PAIRS != kPairsNone) {
                         const float other = PAIRS == kPairsNext ? x[e ^ 1] : PAIRS == kPairsFar ? row_rotated(x[e], 8) : __shfl(x[e], partner);
-                        z[e] = PAIRS == kPairsHalf && 8 * c >= p.rotary ? x[e] : fmaf(other, sn[e], x[e] * cs[e]);
+                        // (a value that is not turned takes nothing of its partner, which may be infinite)
+                        if (PAIRS == kPairsFar || turns) z[e] = fmaf(other, b[e], z[e]);
                     }
-                    if constexpr (PAIRS == kPairsNext) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (8 * c >= p.rotary) z[e] = x[e];      // (not x * 1 + y * 0: y may be infinite)
-                    }
+                    if (NORM) z[e] *= inv;
                 }
-                if (is_q || is_k) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * e], z[2 * e + 1]}, bf16x2));
-                }
+                for (int e = 0; e < 4; ++e)
+                    y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * e], z[2 * e + 1]}, bf16x2));
             }
-            if (quad0 + i >= quad_end || r >= rows) continue;
-            if (is_q) {
-                *reinterpret_cast<u32x4*>(p.q_out + ((int64_t)token * p.n_q_heads + r) * kHeadDim + 8 * c) = y;
+            if (head >= (kind == Q ? p.n_q_heads : p.n_kv_heads)) continue;
+            if (kind == Q) {
+                *reinterpret_cast<u32x4*>(p.q_out + ((int64_t)token * p.n_q_heads + head) * kHeadDim + 8 * c) = y;
             } else if (!APPEND) {
-                *reinterpret_cast<u32x4*>(p.k_out + ((int64_t)token * p.n_kv_heads + r - p.n_q_heads) * kHeadDim + 8 * c) = y;
+                *reinterpret_cast<u32x4*>(p.k_out + ((int64_t)token * p.n_kv_heads + head) * kHeadDim + 8 * c) = y;
             } else {
-                unsigned char* const slot = is_k ? k_slot : v_slot;
-                const int h = r - p.n_q_heads - (is_k ? 0 : p.n_kv_heads);
-                if (slot) *reinterpret_cast<u32x4*>(slot + (int64_t)h * p.cache.head_b + 16 * c) = y;
+                unsigned char* const slot = kind == K ? k_slot : v_slot;
+                if (slot) *reinterpret_cast<u32x4*>(slot + (int64_t)head * p.cache.head_b + 16 * c) = y;
             }
         }
     }

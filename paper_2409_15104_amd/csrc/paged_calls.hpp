@@ -109,8 +109,7 @@ void launch_norm_rope(const NormRopeParams& p, dim3 grid, hipStream_t st) {
 }
 
 int launch_norm_rope(NormRopeParams& p, bool append, hipStream_t st) {
-    const int rows = p.n_q_heads + (append ? 2 : 1) * p.n_kv_heads;
-    p.parts = norm_rope_parts(compute_units(), p.tokens, rows);
+    p.parts = norm_rope_parts(compute_units(), p.tokens, (p.n_q_heads + 3) / 4 + (append ? 2 : 1) * ((p.n_kv_heads + 3) / 4));
     const int64_t waves = (int64_t)p.tokens * p.parts;
     const int64_t blocks = (waves + kNormRopeThreads / 64 - 1) / (kNormRopeThreads / 64);
     if (blocks > 0x7fffffff) return PEC_ERR_UNSUPPORTED;

@@ -249,7 +249,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
         if ((req_tile + 1) * kStepTile <= req.keys) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i)
-                dma16<false>(pool + off[i >> 1] + (i & 1) * 4 * (int64_t)cache.row_b, is_v ? ldv : ldk[i & 3], l0 + i * 1024);
+                dma16_once(pool + off[i >> 1] + (i & 1) * 4 * (int64_t)cache.row_b, is_v ? ldv : ldk[i & 3], l0 + i * 1024);
         } else {      // keys past the end re-read the last one: their weights are zero
             const int last = max(0, req.keys - 1);
 #pragma unroll
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
                 const uint32_t col = is_v ? (uint32_t)((((ld_pos >> 2) ^ (key & 3)) << 2) | (ld_pos & 3)) * 16u
                                           : (uint32_t)(ld_pos ^ (key & 15)) * 16u;
                 const int from = min(req_tile * kStepTile + key, last) - min(req_tile * kStepTile + 8 * (i >> 1), last & ~7);
-                dma16<false>(pool + off[i >> 1], (uint32_t)from * cache.row_b + col, l0 + i * 1024);
+                dma16_once(pool + off[i >> 1], (uint32_t)from * cache.row_b + col, l0 + i * 1024);
             }
         }
     };
