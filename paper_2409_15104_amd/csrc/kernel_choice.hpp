@@ -324,19 +324,64 @@ inline int64_t decode_default_ranges(int cu, int n_q_heads, int n_kv_heads, int6
     return std::max<int64_t>(1, std::min<int64_t>(per_cu, sk / 1024));
 }
 
-// Which kernels a paged call runs on: paged_step_kernel (32 nt rows a unit) for sequences with few rows per KV head, the
-// pipelined kernel's work list for the others.  len_q: new tokens of a sequence at most, as far as the host knows.
+// Which kernels a paged call runs on.  `units`: a workgroup of paged_step_kernel for every 32 rows of a KV head, nothing else;
+// `steps`: its spans and their merge, for sequences with few rows per KV head (32 nt); `list`: the pipelined kernel's work list for
+// the others, or for all.  The host knows no lengths but the caller's hints (len_q, len_k: the longest), so these are estimates
+// for sequences that are all as long, in microseconds, fitted to 40 random calls on 256 compute units.
 constexpr int kPagedFewRows = 64;
 struct PagedCut {
-    bool steps, list;
+    bool units, steps, list;
+    int unit_waves;          // wavefronts of a unit's workgroup
     int nt, few_rows;        // few_rows: rows up to which a sequence goes to the steps where both run
 };
-inline PagedCut paged_cut(int64_t len_q, int64_t batch, int group) {
+// Units: rounds of workgroups of eight wavefronts, or, where there are more of them than compute units, of four with two to a
+// compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end and, per 256 keys, 2 (2.4
+// where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads 16.7 / 14.8; 41 of 5,054, 8 / 2
+// 58 / 59; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
+inline double paged_units(int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q) {
+    return n_kv_heads * (len_q * group <= 32 ? (double)batch : (double)total_q * group / 32 + 0.5 * batch);
+}
+inline double paged_units_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+    const double n = paged_units(group, n_kv_heads, batch, total_q, len_q);
+    const int at_once = n > cu ? 2 * cu : cu;
+    const double per = n > cu ? 3.0 : len_q * group <= 128 ? 2.4 : 2.0;
+    const double longest = per * std::ceil(len_k / 256.0), middle = per * std::max(1.0, (len_k - 0.5 * len_q) / 256.0);
+    return 3 + std::max(6.5 + longest, std::ceil(n / at_once) * (6.5 + middle));
+}
+// The list: 18 for its launches, then rounds of items, 1.4 per 64 keys and eight such steps for an item's ends, in whole walks or
+// in ranges (paged_list_kernel does the same sum with the lengths themselves); 9 more for a launch of steps beside it.  (Two
+// of 1,100, 24 / 8 heads 54 / 58; 1,277 behind 1,140, 32 / 8 80 / 76; 675 behind 4,000, 8 / 2 70 / 77; 953, 5 / 1 50 / 42.)
+inline double paged_list_us(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, bool steps) {
+    const int log_heads = most_log_heads_per_item(n_q_heads, n_kv_heads);
+    const double items = ((double)total_q / (kBM >> log_heads) + 0.5 * batch) * (n_q_heads >> log_heads), walk = len_k / 64.0;
+    double best = std::ceil(items / cu) * (items <= cu ? walk + 8 : walk - len_q / 128.0 + 8);
+    for (int parts = 2; parts <= 64 && walk / parts >= 16; ++parts)
+        best = std::min(best, std::ceil(items * parts / cu) * (walk / parts + 12) + 7);
+    return 18 + 1.4 * best + (steps ? 9 : 0);
+}
+// Spans: 12 for both launches, what memory takes, and the merge, which goes by the steps of a span (least_span()).
+inline double paged_steps_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t len_q, int64_t len_k) {
+    const double rows = std::min((double)kPagedFewRows, (double)len_q * group), keys = (double)batch * len_k * n_kv_heads;
+    const double merge = len_k / 4096.0 + keys / 32 * rows / 3900, own = keys / 32 / (cu * (rows <= 32 ? 8 : 4)), least = std::sqrt(merge / 1.3);
+    return 12 + keys * 512 / 6.0e6 + (own >= least ? merge / own : 2 * 1.3 * least - 1.3 * own);
+}
+// Sequences of very different lengths suit a list and spans, which cut them, and not units: these are taken only where even the
+// longest is short, or alone.
+constexpr int64_t kPagedUnitKeys = 13 * 256;
+inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+    const int g = n_q_heads / n_kv_heads;
     PagedCut c{};
-    c.list = len_q * group > kPagedFewRows;
-    c.few_rows = group <= 32 ? 32 : group <= 64 ? 64 : 0;
-    c.steps = !c.list || (batch > 1 && c.few_rows > 0);
-    c.nt = c.list ? c.few_rows / 32 : len_q * group <= 32 ? 1 : 2;
+    c.list = len_q * g > kPagedFewRows;
+    c.few_rows = g <= 32 ? 32 : g <= 64 ? 64 : 0;
+    // steps beside a list where the longest sequences leave room for more than two with few rows (one or two are items like others)
+    c.steps = !c.list || (c.few_rows > 0 && batch - (total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2);
+    const double units = paged_units_us(cu, g, n_kv_heads, batch, total_q, len_q, len_k);
+    c.units = (batch == 1 || len_k <= kPagedUnitKeys) &&
+              units < (c.list ? paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, c.steps)
+                              : paged_steps_us(cu, g, n_kv_heads, batch, len_q, len_k));
+    if (c.units) c.steps = c.list = false;
+    c.unit_waves = paged_units(g, n_kv_heads, batch, total_q, len_q) > cu ? 4 : 8;
+    c.nt = c.units ? 1 : c.list ? c.few_rows / 32 : len_q * g <= 32 ? 1 : 2;
     return c;
 }
 

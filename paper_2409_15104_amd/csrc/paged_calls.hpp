@@ -71,7 +71,7 @@ PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_
     const size_t rows = std::max((size_t)cu * kPagedWaves1 * 2 * 32, (size_t)l.slots * l.units * kBM);
     l.off_lse = rows * kHeadDim * sizeof(float);
     l.off_prefix = up(l.off_lse + rows * sizeof(float));
-    l.off_work = up(l.off_prefix + ((size_t)batch + 1) * sizeof(int32_t));
+    l.off_work = up(l.off_prefix + ((size_t)batch + 2) * sizeof(int32_t));
     l.off_counters = up(l.off_work + (size_t)l.capacity * sizeof(WorkItem));
     l.off_splits = l.off_counters + 256;
     l.bytes = up(l.off_splits + (size_t)(l.slots / 2 + 1) * sizeof(PagedSplit));
@@ -220,38 +220,59 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
     }
     if (batch->batch > kPagedChunks * 64) return PEC_ERR_UNSUPPORTED;
     const int cu = std::max(8, compute_units() & ~7), g = p.group;
+    if (batch->total_q * g > 0x7fffffff - 64) return PEC_ERR_UNSUPPORTED;      // rows of a KV head
     const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
     const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
     char* const ws = static_cast<char*>(workspace);
-    const PagedCut cut = paged_cut(len_q, batch->batch, g);
+    const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
+    const PagedCut cut = paged_cut(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k);
 
+    if (cut.units) {
+        PagedStepParams s{};
+        s.a = p;
+        s.cut = StepCut{fast_div(g), 5, p.causal, 0x7fffffff};
+        const int64_t groups = (batch->total_q * g / 32 + batch->batch) * p.n_kv_heads;
+        if (groups > 0x7fffff00) return PEC_ERR_UNSUPPORTED;
+        const dim3 grid((unsigned)((groups + 7) / 8 * 8));
+        if (cut.unit_waves == 4)
+            hipLaunchKernelGGL((paged_step_kernel<1, 4, 1, true>), grid, dim3(4 * 64), 0, st, s);
+        else
+            hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1, true>), grid, dim3(kPagedWaves1 * 64), 0, st, s);
+        return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    }
     if (cut.steps) {
         PagedStepParams s{};
         s.a = p;
         s.part_out = reinterpret_cast<float*>(ws);
         s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
         s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-        s.most_rows = cut.list ? cut.few_rows : 0x7fffffff;
+        s.cut = StepCut{fast_div(g), cut.nt == 1 ? 5 : 6, p.causal, cut.list ? cut.few_rows : 0x7fffffff};
         const int waves = cu * (cut.nt == 1 ? kPagedWaves1 : kPagedWaves2);
         if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
-        s.n_spans = waves / p.n_kv_heads;
+        s.n_spans = fast_div(waves / p.n_kv_heads);
+        s.kv_heads = fast_div(p.n_kv_heads);
+        s.unit_rows = (int32_t)std::min<int64_t>(32 * cut.nt, len_q * g);
         // every tile step has a number
         const int64_t per_seq = (std::min<int64_t>(cut.list ? cut.few_rows : len_q * g, len_q * g) + 32 * cut.nt - 1) / (32 * cut.nt);
         const int64_t row_tiles = cut.list ? batch->batch * per_seq : batch->total_q * g / (32 * cut.nt) + batch->batch;
         if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;
         if (cut.nt == 1)
-            hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
+            hipLaunchKernelGGL((paged_step_kernel<1, kPagedWaves1, 1, false>), dim3(cu), dim3(kPagedWaves1 * 64), 0, st, s);
         else
-            hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
+            hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2, false>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
         const int tokens = (int)std::max<int64_t>(1, std::min(len_q, (int64_t)(cut.nt * 32 / g)));
-        const int64_t rows = (int64_t)batch->batch * tokens;
-        if (rows * shape->n_q_heads >= (int64_t)cu * 8)      // rows for every wavefront
-            hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), (unsigned)shape->n_q_heads),
-                               dim3(kPagedMergeThreads), 0, st, s, 32 * cut.nt, tokens);
+        const int64_t rows = (int64_t)batch->batch * tokens, waves_wanted = (int64_t)cu * 8;
+        const unsigned heads = (unsigned)shape->n_q_heads;
+        // pieces of the longest unit, as far as the hints tell: a step each at most, and four times a sequence's share of the spans
+        const int64_t pieces = std::min({len_k / kStepTile, (int64_t)s.n_spans.d, 4 * (int64_t)s.n_spans.d / batch->batch});
+        if (rows * heads >= waves_wanted)
+            hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), heads), dim3(256), 0, st, s,
+                               tokens);
+        else if (pieces < 128 || rows * heads > 512)
+            hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, heads), dim3(256), 0, st, s, tokens);
         else
-            hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, (unsigned)shape->n_q_heads), dim3(kPagedMergeThreads), 0, st, s,
-                               32 * cut.nt, tokens);
+            hipLaunchKernelGGL(paged_merge_kernel<16>, dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     }
     if (!cut.list) return PEC_OK;

@@ -13,6 +13,19 @@ namespace pec {
 
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;   // read-only in a launch: scalar loads
 
+// Division of numbers below 2^31 by one the host knows: a product and a shift (m = floor(2^(31 + l) / d) + 1, l = ceil(log2 d)) in
+// the place of some thirty instructions.  The kernels of small calls are little but address arithmetic.
+struct FastDiv {
+    uint32_t m;
+    int32_t shift, d;
+    __host__ __device__ __forceinline__ int div(int x) const { return (int)((uint64_t)m * (uint32_t)x >> shift); }
+};
+inline FastDiv fast_div(int d) {
+    int l = 0;
+    while (((int64_t)1 << l) < d) ++l;
+    return FastDiv{(uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)d + 1), 31 + l, d};
+}
+
 struct PagedKv {
     unsigned char* k;            // element (page, slot, head, dim) at page_b * page + row_b * slot + head_b * head + 2 * dim bytes
     unsigned char* v;

@@ -30,34 +30,39 @@ constexpr int kStepTile = 32;
 constexpr int kStepTileBytes = kStepTile * kRowBytes;
 constexpr int kPagedChunks = 1024;                     // sequences are added up 64 at a time: up to 65,536 of them
 
+
+// How a call's sequences are cut: R = 2^log_r rows a unit; a sequence has less than 2^31 rows.
+struct StepCut {
+    FastDiv group;
+    int log_r, causal, most_rows;
+    // keys that row tile `rt` of `s` walks, its steps (tiles of 32 keys, at least one), row tiles of s, steps of all of them
+    __device__ __forceinline__ int keys(const PagedSeq& s, int rt) const {
+        if (!causal) return s.len_k;
+        const int last_row = min(s.len_q * group.d, (rt + 1) << log_r) - 1;
+        return max(0, min(s.len_k, s.len_k - s.len_q + group.div(last_row) + 1));
+    }
+    __device__ __forceinline__ int tiles(const PagedSeq& s, int rt) const { return max(1, (keys(s, rt) + kStepTile - 1) / kStepTile); }
+    __device__ __forceinline__ int row_tiles(const PagedSeq& s) const {
+        const int rows = s.len_q * group.d;
+        return rows > most_rows ? 0 : (int)((uint32_t)(rows + (1 << log_r) - 1) >> log_r);
+    }
+    __device__ __forceinline__ int all_tiles(const PagedSeq& s) const {
+        const int n = row_tiles(s);
+        int sum = 0;
+        for (int rt = 0; rt < n; ++rt) sum += tiles(s, rt);
+        return sum;
+    }
+};
 struct PagedStepParams {
     PagedAttnParams a;
     float* part_out;          // [spans][KV heads][2][32 NT][128]
     float* part_lse;          // [spans][KV heads][2][32 NT]
-    int32_t* prefix;          // [batch + 1]: steps of a KV head ahead of each sequence, and of all of them
-    int32_t n_spans;          // of a KV head
-    int32_t most_rows;        // sequences with more rows than this are not this launch's (0x7fffffff: all are)
+    int32_t* prefix;          // [batch + 2]: steps of a KV head ahead of each sequence, and of all of them; the least steps of a span
+    FastDiv n_spans;          // of a KV head
+    FastDiv kv_heads;
+    int32_t unit_rows;        // rows of a unit, as far as the host knows
+    StepCut cut;              // most_rows: sequences with more rows are not this launch's (0x7fffffff: all are)
 };
-
-// Steps (tiles of 32 keys, at least one) of row tile `rt` of `s`, R rows each, and of all of its row tiles.
-__device__ __forceinline__ int step_keys(const PagedSeq& s, int group, int causal, int r, int rt) {
-    if (!causal) return s.len_k;
-    const int64_t rows = min((int64_t)s.len_q * group, (int64_t)(rt + 1) * r);
-    return max(0, min(s.len_k, s.len_k - s.len_q + (int)((rows - 1) / group) + 1));
-}
-__device__ __forceinline__ int step_tiles(const PagedSeq& s, int group, int causal, int r, int rt) {
-    return max(1, (step_keys(s, group, causal, r, rt) + kStepTile - 1) / kStepTile);
-}
-__device__ __forceinline__ int step_row_tiles(const PagedSeq& s, int group, int r, int most_rows) {
-    const int64_t rows = (int64_t)s.len_q * group;
-    return rows > most_rows ? 0 : (int)((rows + r - 1) / r);
-}
-__device__ __forceinline__ int step_tiles_of(const PagedSeq& s, int group, int causal, int r, int most_rows) {
-    const int n = step_row_tiles(s, group, r, most_rows);
-    int sum = 0;
-    for (int rt = 0; rt < n; ++rt) sum += step_tiles(s, group, causal, r, rt);
-    return sum;
-}
 __device__ __forceinline__ int wave_prefix(int x) {      // inclusive
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -67,72 +72,62 @@ __device__ __forceinline__ int wave_prefix(int x) {      // inclusive
     }
     return x;
 }
+// A KV head's line of `total` steps in equal spans of at least `least`: the first `extra` of them have len + 1 steps.
 struct StepSpans {
-    int len, extra;              // the first `extra` spans have len + 1 steps
-    __device__ __forceinline__ StepSpans(int steps, int n_spans) : len(steps / n_spans), extra(steps % n_spans) {}
-    __device__ __forceinline__ int start(int i) const { return i * len + min(i, extra); }
+    int total, len, extra;
+    __device__ __forceinline__ StepSpans(int steps, const FastDiv& n_spans, int least) : total(steps), len(n_spans.div(steps)), extra(0) {
+        if (len >= least) extra = steps - len * n_spans.d;
+        else len = least;
+    }
+    __device__ __forceinline__ int start(int i) const { return (int)min((int64_t)total, (int64_t)i * len + min(i, extra)); }
     __device__ __forceinline__ int of(int step) const {       // the span that the step falls into
         const int head = extra * (len + 1);
         return step < head ? step / (len + 1) : extra + (step - head) / max(1, len);
     }
 };
+// Steps that a span should have at least: a step more takes its wavefront 1.3 us (a trip to memory), while the merge is the
+// shorter the fewer pieces there are, 1 us for 128 of the longest unit's, a step each, and what all rows' pieces take through
+// memory and back at 4 TB/s.  With one step per span 8 sequences x 7 tokens x 5 heads on 1,924 tokens took 33 us and one of
+// 17,126 tokens of 2 KV heads 27.
+__device__ __forceinline__ int least_span(int total, int longest, int n_kv_heads, int unit_rows) {
+    const float merge_us = (float)longest * (1.f / 128.f) + (float)total * (float)(n_kv_heads * unit_rows) * (1.f / 3900.f);
+    return max(1, (int)__builtin_amdgcn_sqrtf(merge_us * (1.f / 1.3f)));
+}
 
-template <int NT, int WAVES, int S>
-__global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedStepParams p) {
-    constexpr int R = 32 * NT;
-    constexpr int LOADS = 8;                 // load instructions (1 KiB each) per matrix and tile
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[WAVES * S * 2 * kStepTileBytes];
-    __shared__ int32_t chunk_sum[kPagedChunks];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    const int l32 = lane & 31, hl = lane >> 5;
-    const int g = p.a.group, causal = p.a.causal;
-
-    // ---- all steps of a KV head, and where this wavefront's span begins.  Up to 64 sequences sit in the lanes of every wavefront.
-    const PagedBatch& bt = p.a.batch;
-    const int n_chunks = (bt.batch + 63) >> 6;
-    auto load = [&](int b) {
+// Sequences laid end to end, `value` of a sequence being its length on that line.  Up to 64 of them sit in the lanes of every
+// wavefront; of more, `chunk_sum` (LDS) keeps the sums of 64 at a time, which the wavefronts share out among themselves.
+template <int WAVES, class Value>
+struct PagedLine {
+    const PagedBatch& bt;
+    const Value value;
+    int32_t* const chunk_sum;
+    const int n_chunks, lane;
+    PagedSeq lanes;
+    int own, upto, total;
+    __device__ __forceinline__ PagedSeq load(int b) const {
         PagedSeq s{0, 0, 0};
         if (b < bt.batch) s = paged_seq(bt, b);
         return s;
-    };
-    auto tiles_of = [&](const PagedSeq& s) { return step_tiles_of(s, g, causal, R, p.most_rows); };
-    PagedSeq lanes = load(lane);
-    int own = tiles_of(lanes), upto = wave_prefix(own), per_head;
-    if (n_chunks <= 1) {
-        per_head = __builtin_amdgcn_readlane(upto, 63);
-    } else {
+    }
+    __device__ __forceinline__ PagedLine(const PagedBatch& batch, Value v, int32_t* sums, int wave)
+        : bt(batch), value(v), chunk_sum(sums), n_chunks((batch.batch + 63) >> 6), lane(threadIdx.x & 63) {
+        lanes = load(lane);
+        own = value(lanes);
+        upto = wave_prefix(own);
+        if (n_chunks <= 1) {
+            total = __builtin_amdgcn_readlane(upto, 63);
+            return;
+        }
         for (int c = wave; c < n_chunks; c += WAVES) {
-            const int sum = wave_prefix(tiles_of(load(64 * c + lane)));
+            const int sum = wave_prefix(value(load(64 * c + lane)));
             if (lane == 63) chunk_sum[c] = sum;
         }
         __syncthreads();
         int sum = 0;
         for (int c = lane; c < n_chunks; c += 64) sum += chunk_sum[c];
-        per_head = __builtin_amdgcn_readlane(wave_prefix(sum), 63);
+        total = __builtin_amdgcn_readlane(wave_prefix(sum), 63);
     }
-    if (blockIdx.x == 0) {       // for the merge
-        for (int c = wave, ahead = 0, at = 0; c < n_chunks; c += WAVES) {
-            for (; at < c; ++at) ahead += chunk_sum[at];
-            const int mine = tiles_of(load(64 * c + lane)), all = wave_prefix(mine);
-            if (64 * c + lane < bt.batch) p.prefix[64 * c + lane] = ahead + all - mine;
-        }
-        if (threadIdx.x == 0) p.prefix[bt.batch] = per_head;
-    }
-    if (per_head == 0) return;
-    const StepSpans spans(per_head, p.n_spans);
-    const int group_no = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);     // neighbours on one XCD
-    const int w = group_no * WAVES + wave, span = w / p.a.n_kv_heads, kvh = w % p.a.n_kv_heads;
-    const int start = spans.start(span);
-    int left = span < p.n_spans ? spans.start(span + 1) - start : 0;       // tiles to work on
-    if (left <= 0) return;
-
-    // Row tile `rt` of sequence `seq`; uniform.
-    struct Unit {
-        PagedSeq s;
-        int seq, rt, row0, rows, keys, tiles;
-    };
-    auto seq_of = [&](int i) {
+    __device__ __forceinline__ PagedSeq seq(int i) const {       // uniform
         PagedSeq s;
         if (n_chunks <= 1) {
             s.q0 = __builtin_amdgcn_readlane(lanes.q0, i);
@@ -140,39 +135,19 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
             s.len_k = __builtin_amdgcn_readlane(lanes.len_k, i);
         } else {
             s = paged_seq(bt, i);
+            s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
+            s.len_q = __builtin_amdgcn_readfirstlane(s.len_q);
+            s.len_k = __builtin_amdgcn_readfirstlane(s.len_k);
         }
         return s;
-    };
-    auto unit_of = [&](const PagedSeq& s, int seq, int rt) {
-        Unit u;
-        u.s = s;
-        u.seq = seq;
-        u.rt = rt;
-        u.row0 = rt * R;
-        u.rows = (int)min((int64_t)R, (int64_t)s.len_q * g - u.row0);
-        u.keys = step_keys(s, g, causal, R, rt);
-        u.tiles = max(1, (u.keys + kStepTile - 1) / kStepTile);
-        return u;
-    };
-    auto next_unit = [&](const Unit& u) {
-        PagedSeq s = u.s;
-        int seq = u.seq, rt = u.rt + 1;
-        while (rt >= step_row_tiles(s, g, R, p.most_rows)) {
-            rt = 0;
-            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch)
-                seq = 0;
-                break;
-            }
-            s = seq_of(seq);
-        }
-        return unit_of(s, seq, rt);
-    };
-    Unit unit;
-    int tile;
-    {
-        int at = start, c0 = 0;
-        if (n_chunks > 1) {              // the chunk of 64 sequences
+    }
+    // The sequence that point `at` < total falls into, `at` becoming its place there; -1: none (never, unless the offsets change
+    // under the launch).
+    __device__ __forceinline__ int find(int& at) {
+        int c0 = 0;
+        if (n_chunks > 1) {
             for (;; c0 += 64) {
+                if (c0 >= n_chunks) return -1;
                 const int sum = c0 + lane < n_chunks ? chunk_sum[c0 + lane] : 0, all = wave_prefix(sum);
                 const uint64_t behind = __ballot(all > at);
                 if (behind != 0) {
@@ -184,25 +159,134 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
                 at -= __shfl(all, 63);
             }
             c0 = __builtin_amdgcn_readfirstlane(c0);
-            own = tiles_of(load(64 * c0 + lane));
+            own = value(load(64 * c0 + lane));
             upto = wave_prefix(own);
         }
-        const uint64_t behind = __ballot(upto > at);     // the sequence
-        if (behind == 0) return;         // (never, unless the offsets change under the launch)
+        const uint64_t behind = __ballot(upto > at);
+        if (behind == 0) return -1;
         const int l = __builtin_ctzll(behind);
         at = __builtin_amdgcn_readfirstlane(at - __builtin_amdgcn_readlane(upto, l) + __builtin_amdgcn_readlane(own, l));
-        const int seq = 64 * c0 + l;
-        const PagedSeq s = seq_of(seq);
-        const int n_rt = step_row_tiles(s, g, R, p.most_rows);
-        int rt = 0;                      // the row tile
-        for (; rt < n_rt; ++rt) {
-            const int n = step_tiles(s, g, causal, R, rt);
-            if (at < n) break;
-            at -= n;
+        return 64 * c0 + l;
+    }
+};
+
+// Two ways to share out the work.  Spans (SHARED = false), as above.  Units (SHARED = true), for calls that are small all over:
+// a workgroup per unit, whose wavefronts take every WAVES-th of its tiles and join their results in LDS; no workspace and no
+// second launch, but nothing evens out units of different lengths.
+template <int NT, int WAVES, int S, bool SHARED>
+__global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedStepParams p) {
+    constexpr int R = 32 * NT;
+    constexpr int LOADS = 8;                 // load instructions (1 KiB each) per matrix and tile
+    constexpr int STRIDE = SHARED ? WAVES : 1;
+    constexpr int kStageBytes = WAVES * S * 2 * kStepTileBytes;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStageBytes];
+    __shared__ int32_t chunk_sum[kPagedChunks];
+    __shared__ float joint[SHARED ? 3 * WAVES * 32 : 1];
+    static_assert(!SHARED || kStageBytes >= WAVES * 32 * kHeadDim * (int)sizeof(float), "the wavefronts' O of 32 rows is joined there");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int l32 = lane & 31, hl = lane >> 5;
+    const int g = p.a.group, causal = p.a.causal;
+    const StepCut& cut = p.cut;
+    const PagedBatch& bt = p.a.batch;
+
+    auto length = [&](const PagedSeq& s) {
+        return SHARED ? cut.row_tiles(s) : cut.all_tiles(s);
+    };
+    PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
+    if (!SHARED && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
+        for (int c = wave, ahead = 0, at = 0; c < line.n_chunks; c += WAVES) {
+            for (; at < c; ++at) ahead += chunk_sum[at];
+            const int mine = length(line.load(64 * c + lane)), all = wave_prefix(mine);
+            if (64 * c + lane < bt.batch) p.prefix[64 * c + lane] = ahead + all - mine;
         }
-        if (rt >= n_rt) return;          // (the same)
+        if (threadIdx.x == 0) p.prefix[bt.batch] = line.total;
+    }
+    if (line.total == 0) return;
+    int least = 1;
+    if constexpr (!SHARED) {
+        int longest = line.total / 64;       // (of more than 64 sequences: that many alike)
+        if (line.n_chunks <= 1) {
+            longest = cut.row_tiles(line.lanes) > 0 ? (line.lanes.len_k + kStepTile - 1) / kStepTile : 0;
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off));
+        }
+        least = __builtin_amdgcn_readfirstlane(least_span(line.total, longest, p.a.n_kv_heads, p.unit_rows));
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.prefix[bt.batch + 1] = least;
+    }
+    int at, left, kvh, w = 0;               // place on the line, tiles to work on
+    if constexpr (SHARED) {
+        const WorkOrder order(line.total, 1, p.a.n_kv_heads);
+        if ((blockIdx.x >> 3) >= order.count) return;
+        const int64_t unit = order.unit(blockIdx.x & 7, blockIdx.x >> 3);
+        if (unit < 0) return;
+        kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
+        at = __builtin_amdgcn_readfirstlane((int)unit - kvh * line.total);
+    } else {
+        const StepSpans spans(line.total, p.n_spans, least);
+        // Neighbouring heads and spans on neighbouring wavefronts of one XCD; but short spans on as many compute units as there
+        // are, whose memory paths are what a few tiles take (4 sequences of 540 tokens 14.4 -> 11.7 us, while 4 of 107,000
+        // would take 288 instead of 277).
+        const int group_no = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+        w = spans.len < 8 ? wave * (int)gridDim.x + (int)blockIdx.x : group_no * WAVES + wave;
+        const int span = p.kv_heads.div(w);
+        kvh = w - span * p.a.n_kv_heads;
+        at = spans.start(span);
+        left = span < p.n_spans.d ? spans.start(span + 1) - at : 0;
+        if (left <= 0) return;
+    }
+
+    // Row tile `rt` of sequence `seq`; uniform.
+    struct Unit {
+        PagedSeq s;
+        int seq, rt, row0, rows, keys, tiles;
+    };
+    auto unit_of = [&](const PagedSeq& s, int seq, int rt) {
+        Unit u;
+        u.s = s;
+        u.seq = seq;
+        u.rt = rt;
+        u.row0 = rt * R;
+        u.rows = min(R, s.len_q * g - u.row0);
+        u.keys = cut.keys(s, rt);
+        u.tiles = max(SHARED ? 0 : 1, (u.keys + kStepTile - 1) / kStepTile);
+        return u;
+    };
+    auto next_unit = [&](const Unit& u) {
+        PagedSeq s = u.s;
+        int seq = u.seq, rt = u.rt + 1;
+        while (rt >= cut.row_tiles(s)) {
+            rt = 0;
+            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch)
+                seq = 0;
+                break;
+            }
+            s = line.seq(seq);
+        }
+        return unit_of(s, seq, rt);
+    };
+    Unit unit;
+    int tile;
+    {
+        const int seq = __builtin_amdgcn_readfirstlane(line.find(at));
+        if (seq < 0) return;
+        at = __builtin_amdgcn_readfirstlane(at);
+        const PagedSeq s = line.seq(seq);
+        const int n_rt = cut.row_tiles(s);
+        int rt = 0;
+        if constexpr (SHARED) {
+            rt = n_rt - 1 - at;              // the longest first
+        } else {
+            for (; rt < n_rt; ++rt) {
+                const int n = cut.tiles(s, rt);
+                if (at < n) break;
+                at -= n;
+            }
+        }
+        if (rt < 0 || rt >= n_rt) return;    // (never, as above)
         unit = unit_of(s, seq, rt);
-        tile = at;
+        tile = SHARED ? wave : at;
+        if constexpr (SHARED) left = max(0, (unit.tiles - wave + WAVES - 1) / WAVES);
     }
 
     // ---- lane constants of the tile loads and operand reads
@@ -228,59 +312,43 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     Unit req = unit;
     int req_tile = tile, req_left = left;
     const int64_t head_off = (int64_t)kvh * cache.head_b;
-    uint32_t number[4];      // page numbers of its four groups of eight keys (keys past the end: the last key's),
+    uint32_t number[4];      // page numbers of its four groups of eight keys (of keys past the end: the last key's),
     int64_t off[4];          // and byte offsets of the groups
     auto look_up = [&]() {
-        if (req.keys == 0) return;
         const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)req.seq * bt.table_len);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) number[i] = (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
+        for (int i = 0; i < 4; ++i) number[i] = req.keys == 0 ? 0 : (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
     };
     auto locate = [&]() {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int key = min(req_tile * kStepTile + 8 * i, (req.keys - 1) & ~7);
-            off[i] = min(number[i], cache.last_page) * cache.page_b + (uint64_t)(uint32_t)(key & ((1 << cache.log_page) - 1)) * cache.row_b + head_off;
+            const uint32_t slot = (uint32_t)(req_tile * kStepTile + 8 * i) & ((1u << cache.log_page) - 1);
+            off[i] = min(number[i], cache.last_page) * cache.page_b + (uint64_t)slot * cache.row_b + head_off;
         }
     };
-    // (a unit without keys is one tile whose loads fetch whatever is at the start of the cache; everything of it is masked)
+    // Keys past the end come along, from the slots behind the last one or from whatever page is at hand: their scores are masked
+    // and their values zeroed in LDS.
     auto issue = [&](const unsigned char* pool, bool is_v, unsigned char* stage) {
         const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)stage;
-        if ((req_tile + 1) * kStepTile <= req.keys) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                dma16_once(pool + off[i >> 1] + (i & 1) * 4 * (int64_t)cache.row_b, is_v ? ldv : ldk[i & 3], l0 + i * 1024);
-        } else {      // keys past the end re-read the last one: their weights are zero
-            const int last = max(0, req.keys - 1);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int key = 4 * i + ld_row;
-                const uint32_t col = is_v ? (uint32_t)((((ld_pos >> 2) ^ (key & 3)) << 2) | (ld_pos & 3)) * 16u
-                                          : (uint32_t)(ld_pos ^ (key & 15)) * 16u;
-                const int from = min(req_tile * kStepTile + key, last) - min(req_tile * kStepTile + 8 * (i >> 1), last & ~7);
-                dma16_once(pool + off[i >> 1], (uint32_t)from * cache.row_b + col, l0 + i * 1024);
-            }
-        }
+        for (int i = 0; i < LOADS; ++i)
+            dma16_once(pool + off[i >> 1] + (i & 1) * 4 * (int64_t)cache.row_b, is_v ? ldv : ldk[i & 3], l0 + i * 1024);
     };
     auto request_k = [&](unsigned char* stage) {
-        if (req.keys == 0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) off[i] = 0;
-        } else {
-            locate();
-        }
+        locate();
         issue(cache.k, false, stage);
     };
     auto request_v = [&](unsigned char* stage) {
         issue(cache.v, true, stage);
         if (--req_left == 0) return;
-        if (++req_tile == req.tiles) {
+        req_tile += STRIDE;
+        if (!SHARED && req_tile == req.tiles) {
             req = next_unit(req);
             req_tile = 0;
         }
         look_up();
     };
-    look_up();
+    if (req_left > 0) look_up();
     int n = 0;               // tiles behind this wavefront, which stage j % S goes by
 #pragma unroll
     for (int i = 0; i < S; ++i)
@@ -292,18 +360,22 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     for (;;) {
         // ---- a piece: tiles [tile, end) of the unit
         const int row0 = unit.row0, rows = unit.rows, keys = unit.keys, last = keys - 1;
-        const int piece0 = tile, end = min(unit.tiles, tile + left);
-        const int first_vis = causal ? unit.s.len_k - unit.s.len_q + row0 / g : last;       // last key of the first row
-        int last_vis[NT];                                                                  // ... of this lane's rows
+        const int piece0 = tile, end = SHARED ? unit.tiles : min(unit.tiles, tile + left);
+        const int first_vis = causal ? unit.s.len_k - unit.s.len_q + cut.group.div(row0) : last;       // last key of the first row
+        int pos[NT], head[NT], last_vis[NT];      // new token, query head and last key of this lane's rows
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + (row0 + nt * 32 + l32) / g) : last;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = row0 + nt * 32 + l32;
+            pos[nt] = cut.group.div(r);
+            head[nt] = kvh * g + r - pos[nt] * g;
+            last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + pos[nt]) : last;
+        }
 
         // ---- Q fragments: rows without a query stay zero and are not stored
         bf16x8 qf[NT][8];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = row0 + nt * 32 + l32;
-            const __bf16* qrow = p.a.q + (unit.s.q0 + r / g) * p.a.q_stride + ((int64_t)kvh * g + r % g) * kHeadDim + 8 * hl;
+            const __bf16* qrow = p.a.q + (unit.s.q0 + pos[nt]) * p.a.q_stride + (int64_t)head[nt] * kHeadDim + 8 * hl;
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 u32x4 raw = {0u, 0u, 0u, 0u};
@@ -327,7 +399,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int t = 0; t < 8; ++t) asm volatile("" : "+v"(qf[nt][t]));
-        for (; tile < end; ++tile, ++n) {
+        for (; tile < end; tile += STRIDE, ++n) {
             const int ahead = --left;           // tiles of the span behind this one
             const int key0 = tile * kStepTile;
             unsigned char *const kst = k_stage(n), *const vst = v_stage(n);
@@ -403,6 +475,13 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
                 else if (ahead == 1) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
+            if (key0 + kStepTile > keys) {      // values past the end: zero
+                const u32x4 z = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i)
+                    if (key0 + 4 * i + ld_row >= keys) *reinterpret_cast<u32x4*>(vst + i * 1024 + lane * 16) = z;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
             // A value that some of the rows do not see reaches them as 0 x value, which an infinite or NaN one is not.  In
             // tiles that hold such keys these values are added by hand to the rows that see them and zeroed for the product.
             if (min(key0 + kStepTile - 1, last) > first_vis) {
@@ -463,6 +542,69 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
             if (ahead >= S) request_v(vst);
         }
 
+        if constexpr (SHARED) {
+            // ---- the wavefronts' results of every row are joined, 32 rows at a time.  O goes to LDS in 16-byte chunks of 4
+            // dims, chunk c of row r at slot c * 32 + (r ^ c): the writers (fixed c, one row per lane) and the readers (fixed
+            // row, one chunk per lane, so that a row leaves as one 256- or 512-byte run) touch all banks evenly.
+            float *const join_m = joint, *const join_l = joint + WAVES * 32, *const join_w = joint + 2 * WAVES * 32;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                __syncthreads();
+                const float l_tot = l_run[nt] + __shfl_xor(l_run[nt], 32);
+                if (hl == 0) {
+                    join_m[wave * 32 + l32] = m_run[nt];
+                    join_l[wave * 32 + l32] = l_tot;
+                }
+                f32x4* const po = reinterpret_cast<f32x4*>(lds) + wave * 1024;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int c = 8 * dt + 2 * b + hl;
+                        f32x4 x;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = o[nt][dt][4 * b + i];
+                        po[c * 32 + (l32 ^ c)] = x;
+                    }
+                __syncthreads();
+                if (threadIdx.x < WAVES * 32) {   // one thread per (row, wavefront): the wavefront's weight
+                    const int r = threadIdx.x & 31, k = threadIdx.x >> 5;
+                    float mx = -INFINITY, den = 0.f;
+#pragma unroll
+                    for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, join_m[i * 32 + r]);
+                    const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+                    for (int i = 0; i < WAVES; ++i) den += join_l[i * 32 + r] * __builtin_amdgcn_exp2f(join_m[i * 32 + r] - ref);
+                    const float inv = den == 0.f ? 0.f : 1.f / den;
+                    join_w[k * 32 + r] = __builtin_amdgcn_exp2f(join_m[k * 32 + r] - ref) * inv;
+                    const int flat = row0 + nt * 32 + r, at_pos = cut.group.div(flat);
+                    if (k == 0 && nt * 32 + r < rows)
+                        p.a.lse[(int64_t)(kvh * g + flat - at_pos * g) * bt.total_q + unit.s.q0 + at_pos] =
+                            den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
+                }
+                __syncthreads();
+                const int c = threadIdx.x & 31;
+#pragma unroll
+                for (int pass = 0; pass < 16 / WAVES; ++pass) {
+                    const int r = pass * 2 * WAVES + (threadIdx.x >> 5), flat = row0 + nt * 32 + r, at_pos = cut.group.div(flat);
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < WAVES; ++k) {
+                        const float wgt = join_w[k * 32 + r];
+                        const f32x4 y = reinterpret_cast<const f32x4*>(lds)[k * 1024 + c * 32 + (r ^ c)];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = fmaf(wgt, y[i], x[i]);
+                    }
+                    if (nt * 32 + r < rows) {
+                        const int64_t idx = ((int64_t)(unit.s.q0 + at_pos) * p.a.n_q_heads + kvh * g + flat - at_pos * g) * kHeadDim + 4 * c;
+                        if (p.a.out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.a.out) + idx) = x;
+                        else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(x, bf16x4);
+                    }
+                }
+            }
+            return;
+        }
+
         // ---- the unit's result, or the piece's into its slot
         const bool whole = piece0 == 0 && end == unit.tiles;
         const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
@@ -470,15 +612,15 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
         for (int nt = 0; nt < NT; ++nt) {
             const float l_tot = l_run[nt] + __shfl_xor(l_run[nt], 32);
             if (nt * 32 + l32 < rows) {
-                const int r = row0 + nt * 32 + l32, head = kvh * g + r % g, token = unit.s.q0 + r / g;
+                const int token = unit.s.q0 + pos[nt];
                 const bool none = l_tot == 0.f || keys == 0;       // (without keys the values may be anything, and the sums NaN)
                 const float inv = none ? 0.f : 1.f / l_tot;
                 const float lse = none ? -INFINITY : (m_run[nt] + __builtin_amdgcn_logf(l_tot)) * kLn2;     // NaN from NaN weights
                 if (hl == 0) {
-                    if (whole) p.a.lse[(int64_t)head * bt.total_q + token] = lse;
+                    if (whole) p.a.lse[(int64_t)head[nt] * bt.total_q + token] = lse;
                     else p.part_lse[slot_row + nt * 32 + l32] = lse;
                 }
-                const int64_t at = whole ? ((int64_t)token * p.a.n_q_heads + head) * kHeadDim : (slot_row + nt * 32 + l32) * kHeadDim;
+                const int64_t at = whole ? ((int64_t)token * p.a.n_q_heads + head[nt]) * kHeadDim : (slot_row + nt * 32 + l32) * kHeadDim;
                 float* const dst = whole ? static_cast<float*>(p.a.out) : p.part_out;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt)
@@ -513,31 +655,30 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
 // Merges the pieces of units that spans have cut: O = sum_i O_i exp(lse_i - L), L = ln sum_i exp(lse_i).  A few KB per row, so
 // trips to memory are all there is to it: a half wavefront per piece, four dims a lane, with a running maximum of its own, four
 // pieces requested at once.  WAVES wavefronts share a row (a new token of a query head): one where there are rows for every
-// wavefront of the chip, which leaves no barrier between them, four where there are fewer and more pieces each.  `tokens`:
-// workgroups per sequence and query head (times four for WAVES = 1), which share its new tokens.
-constexpr int kPagedMergeThreads = 256;
+// wavefront of the chip, which leaves no barrier between them, four or sixteen where there are fewer and more pieces each.
+// `tokens`: workgroups per sequence and query head (times four for WAVES = 1), which share its new tokens.
 template <int WAVES>
-__global__ __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedStepParams p, int r_unit, int tokens) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_kernel(const PagedStepParams p, int tokens) {
     constexpr int N = 2 * WAVES, AHEAD = 4;
     __shared__ __attribute__((aligned(16))) float red[N][kHeadDim];
     __shared__ float red_mx[N], red_den[N];
     const PagedBatch& bt = p.a.batch;
-    const int g = p.a.group, head = blockIdx.y, kvh = head / g, grp = (threadIdx.x >> 5) % N, c = threadIdx.x & 31;
-    const int per_head = p.prefix[bt.batch];
+    const int g = p.a.group, head = blockIdx.y, kvh = p.cut.group.div(head), in_group = head - kvh * g, log_r = p.cut.log_r, grp = (int)(threadIdx.x >> 5) % N, c = threadIdx.x & 31;
+    const int per_head = p.prefix[bt.batch], least = p.prefix[bt.batch + 1];
     constexpr int PER_GROUP = WAVES == 1 ? 4 : 1;       // rows a workgroup works on at a time
     for (int x = blockIdx.x * PER_GROUP + (WAVES == 1 ? (int)(threadIdx.x >> 6) : 0); x < bt.batch * tokens; x += gridDim.x * PER_GROUP) {
         const int seq = x / tokens;
         const PagedSeq s = paged_seq(bt, seq);
-        const int before = p.prefix[seq], n_rt = step_row_tiles(s, g, r_unit, p.most_rows);
+        const int before = p.prefix[seq], n_rt = p.cut.row_tiles(s);
         if (per_head == 0 || n_rt == 0) continue;
-        const StepSpans spans(per_head, p.n_spans);
+        const StepSpans spans(per_head, p.n_spans, least);
         int rt = 0, at = before;       // the row tile in hand, and its first step
         for (int pos = x % tokens; pos < s.len_q; pos += tokens) {
-            const int64_t flat = (int64_t)pos * g + head % g;
-            for (; rt < (int)(flat / r_unit); ++rt) at += step_tiles(s, g, p.a.causal, r_unit, rt);
-            const int w0 = spans.of(at), w1 = spans.of(at + step_tiles(s, g, p.a.causal, r_unit, rt) - 1);
+            const int flat = pos * g + in_group;
+            for (; rt < flat >> log_r; ++rt) at += p.cut.tiles(s, rt);
+            const int w0 = spans.of(at), w1 = spans.of(at + p.cut.tiles(s, rt) - 1);
             if (w0 == w1) continue;
-            const int row = (int)(flat - (int64_t)rt * r_unit);
+            const int row = flat - (rt << log_r);
             float mx = -INFINITY, den = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             for (int w = w0 + grp; w <= w1; w += AHEAD * N) {
@@ -548,7 +689,7 @@ __global__ __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const P
                     l[i] = -INFINITY;
                     o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if (w + i * N <= w1) {
-                        const int64_t slot_row = (((int64_t)(w + i * N) * p.a.n_kv_heads + kvh) * 2 + (w + i * N == w0 ? 1 : 0)) * r_unit + row;
+                        const int64_t slot_row = ((((int64_t)(w + i * N) * p.a.n_kv_heads + kvh) * 2 + (w + i * N == w0 ? 1 : 0)) << log_r) + row;
                         l[i] = p.part_lse[slot_row];
                         o[i] = *reinterpret_cast<const f32x4*>(p.part_out + slot_row * kHeadDim + 4 * c);
                     }
