@@ -280,6 +280,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
     PagedListParams w{};
     w.batch = p.batch;
     w.bm = l.bm;
+    w.log_bm = 8 - l.log_heads;
     w.group = g;
     w.units = l.units;
     w.causal = p.causal;
@@ -324,7 +325,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
     hipLaunchKernelGGL(fwd_il_kernel<kFwdPaged>, dim3((unsigned)groups), dim3(512), 0, st, f);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     if (l.slots > 1) {
-        hipLaunchKernelGGL(paged_ranges_merge_kernel, dim3((unsigned)std::min<int64_t>(l.slots / 2, 64), (unsigned)l.units, 8), dim3(256), 0, st, w,
+        hipLaunchKernelGGL(paged_ranges_merge_kernel, dim3((unsigned)std::min<int64_t>(l.slots / 2 * l.units * 32, 4 * cu)), dim3(256), 0, st, w,
                            f.part_out, f.part_lse, l.log_heads, p.n_q_heads, p.out_f32, out, lse);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     }

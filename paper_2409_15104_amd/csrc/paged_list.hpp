@@ -19,7 +19,7 @@ struct PagedSplit {      // a query tile whose keys are cut into ranges
 };
 struct PagedListParams {
     PagedBatch batch;
-    int32_t bm, group, units, causal;        // positions per item; units of an item, over all KV heads
+    int32_t bm, log_bm, group, units, causal;        // positions per item; units of an item, over all KV heads
     int32_t few_rows;                        // sequences with at most so many rows per KV head are another launch's
     int32_t capacity, slot_capacity, cu;
     WorkItem* work;
@@ -31,23 +31,22 @@ constexpr int kPagedListSeqs = 1024, kPagedListBuckets = 1024;
 
 // Keys that tile t of the sequence walks, and the first of its tiles that walks more than x.
 struct PagedTiles {
-    int n, len_q, len_k, bm, causal;
-    __device__ __forceinline__ PagedTiles(const PagedSeq& s, const PagedListParams& p) : len_q(s.len_q), len_k(s.len_k), bm(p.bm), causal(p.causal) {
-        n = (int64_t)len_q * p.group > p.few_rows ? (len_q + bm - 1) / bm : 0;
+    int n, len_q, len_k, log_bm, causal;
+    __device__ __forceinline__ PagedTiles(const PagedSeq& s, const PagedListParams& p)
+        : len_q(s.len_q), len_k(s.len_k), log_bm(p.log_bm), causal(p.causal) {
+        n = len_q * p.group > p.few_rows ? (int)((uint32_t)(len_q + p.bm - 1) >> log_bm) : 0;      // (rows are below 2^31)
     }
-    __device__ __forceinline__ int keys(int t) const {
-        return causal ? max(0, len_k - len_q + (int)min((int64_t)len_q, (int64_t)(t + 1) * bm)) : len_k;
-    }
+    __device__ __forceinline__ int keys(int t) const { return causal ? max(0, len_k - len_q + min(len_q, (t + 1) << log_bm)) : len_k; }
     __device__ __forceinline__ int first_beyond(int x) const {
         if (len_k <= x) return n;
         const int y = x - (len_k - len_q);
-        return causal && y > 0 ? min(n - 1, y / bm) : 0;
+        return causal && y > 0 ? min(n - 1, y >> log_bm) : 0;
     }
-    // items of all tiles with ranges of `range` keys, and how many tiles are not cut
-    __device__ __forceinline__ int items(int range, int* uncut) const {
-        *uncut = first_beyond(range);
-        int sum = n;
-        for (int64_t x = range; x < len_k; x += range) sum += n - first_beyond((int)x);
+    // Items of all tiles with ranges of `range` keys, and how many tiles are not cut: this lane's share of the sum, the ranges
+    // from number `first` on, every `step`-th.
+    __device__ __forceinline__ int items(int range, int first, int step) const {
+        int sum = first == 0 ? n : 0;
+        for (int64_t x = (int64_t)range * (first == 0 ? step : first); x < len_k; x += (int64_t)range * step) sum += n - first_beyond((int)x);
         return sum;
     }
 };
@@ -90,12 +89,14 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         const int steps = max(16, (whole + parts - 1) / parts), range = wave == 0 || p.slot_capacity == 0 ? 0x40000000 : steps * kBN;
         int64_t all_keys = 0;
         int items = 0, uncut = 0, tiles = 0;
-        for (int b = lane; b < bt.batch; b += 64) {
+        // a lane per sequence, or, of up to eight sequences, eight lanes that share its ranges
+        const int per = bt.batch <= 8 ? 8 : 1, sub = lane % per;
+        for (int b = lane / per; b < bt.batch; b += 64 / per) {
             const PagedTiles t(paged_seq(bt, b), p);
             if (t.n == 0) continue;
-            int u;
-            items += t.items(range, &u);
-            uncut += u;
+            items += t.items(range, sub, per);
+            if (sub != 0) continue;
+            uncut += t.first_beyond(range);
             tiles += t.n;
             all_keys += ((int64_t)t.keys(0) + t.keys(t.n - 1)) * t.n / 2;
         }
@@ -135,9 +136,8 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         if (b >= bt.batch) return;
         Seq q;
         q.s = paged_seq(bt, b);
-        int u;
         const PagedTiles t(q.s, p);
-        q.n_items = t.n > 0 ? t.items(range, &u) : 0;
+        q.n_items = t.n > 0 ? t.items(range, 0, 1) : 0;
         seqs[tid] = q;
     };
     auto bucket_of = [&](const Seq& q) {
@@ -188,41 +188,60 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
     if (tid == 0) p.counters[2] = n_split;
 }
 
-// Merges the ranges of split tiles, 32 rows (those of a wavefront of fwd_il_kernel) per workgroup: grid (split tiles at most,
-// units of an item, 8).
+// Merges the ranges of split tiles, a row per half wavefront, eight rows per workgroup at a time, four ranges requested at once.  A
+// row is latency (28 ranges: seven trips), so rows are spread as wide as they go: 3 x 118 new tokens behind 30,000, 2 / 2 heads, 88 us
+// per call with 32 rows per workgroup, 66 with eight.
 __global__ __launch_bounds__(256) void paged_ranges_merge_kernel(const PagedListParams p, const float* part_out, const float* part_lse,
                                                                  int log_heads, int n_q_heads, int out_f32, void* out, float* lse) {
-    const int n_split = p.counters[2], unit = blockIdx.y, strip = blockIdx.z;
-    const int per_kvh = p.group >> log_heads, kvh = unit / per_kvh, u = unit % per_kvh;
-    const int head = kvh * p.group + (u << log_heads) + (strip >> (3 - log_heads)), c = threadIdx.x & 31;
-    for (int i = blockIdx.x; i < n_split; i += gridDim.x) {
-        const PagedSplit sp = p.splits[i];
+    constexpr int AHEAD = 4;
+    const int n_split = p.counters[2], per_kvh = p.group >> log_heads, c = threadIdx.x & 31;
+    for (int i = blockIdx.x; i < n_split * p.units * 32; i += gridDim.x) {      // (slots are few: this is far below 2^31)
+        const int split = i / (p.units * 32), unit = (i >> 5) % p.units, row = (i & 31) * 8 + (threadIdx.x >> 5), strip = row >> 5;
+        const int kvh = unit / per_kvh, u = unit - kvh * per_kvh;
+        const int head = kvh * p.group + (u << log_heads) + (strip >> (3 - log_heads));
+        const PagedSplit sp = p.splits[split];
         const PagedSeq s = paged_seq(p.batch, sp.seq);
-        const int pos0 = sp.qtile * p.bm + ((strip << 5) & (p.bm - 1));
-        for (int r = threadIdx.x >> 5; r < 32; r += 8) {
-            if (pos0 + r >= s.len_q) break;
-            auto row_of = [&](int n) { return ((int64_t)(sp.slot0 + n) * p.units + unit) * 256 + strip * 32 + r; };
-            float mx = -INFINITY, den = 0.f;
-            for (int n = 0; n < sp.n_ranges; ++n) mx = fmaxf(mx, part_lse[row_of(n)]);      // (NaN: as if it were not there)
-            const float ref = mx == -INFINITY ? 0.f : mx;
-            f32x4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-            for (int n = 0; n < sp.n_ranges; ++n) {
-                const int64_t at = row_of(n);
-                const float w = expf(part_lse[at] - ref);
-                const f32x4 x = *reinterpret_cast<const f32x4*>(part_out + at * kHeadDim + 4 * c);
+        const int pos = sp.qtile * p.bm + ((strip << 5) & (p.bm - 1)) + (row & 31);
+        if (pos >= s.len_q) continue;
+        const int64_t first = ((int64_t)sp.slot0 * p.units + unit) * 256 + row, step = (int64_t)p.units * 256;
+        float mx = -INFINITY, den = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int n0 = 0; n0 < sp.n_ranges; n0 += AHEAD) {
+            float l[AHEAD];
+            f32x4 o[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                l[k] = -INFINITY;
+                o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (n0 + k < sp.n_ranges) {
+                    const int64_t at = first + (n0 + k) * step;
+                    l[k] = part_lse[at];
+                    o[k] = *reinterpret_cast<const f32x4*>(part_out + at * kHeadDim + 4 * c);
+                }
+            }
+            float top = mx;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, l[k]);      // (NaN: as if it were not there)
+            const float ref = top == -INFINITY ? 0.f : top, alpha = expf(mx - ref);
+            den *= alpha;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const float w = expf(l[k] - ref);
                 den += w;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = fmaf(w, x[e], a[e]);
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, o[k][e], acc[e]);
             }
-            const float inv = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] *= inv;
-            const int64_t token = s.q0 + pos0 + r, idx = (token * n_q_heads + head) * kHeadDim + 4 * c;
-            if (out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + idx) = a;
-            else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + idx) = __builtin_convertvector(a, bf16x4);
-            if (c == 0) lse[(int64_t)head * p.batch.total_q + token] = den == 0.f ? -INFINITY : ref + logf(den);
+            mx = top;
         }
+        const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= inv;
+        const int64_t token = s.q0 + pos, idx = (token * n_q_heads + head) * kHeadDim + 4 * c;
+        if (out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + idx) = acc;
+        else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + idx) = __builtin_convertvector(acc, bf16x4);
+        if (c == 0) lse[(int64_t)head * p.batch.total_q + token] = den == 0.f ? -INFINITY : mx + logf(den);
     }
 }
 
