@@ -335,18 +335,19 @@ struct PagedCut {
     int nt, few_rows;        // few_rows: rows up to which a sequence goes to the steps where both run
 };
 // Units: rounds of workgroups of eight wavefronts, or, where there are more of them than compute units, of four with two to a
-// compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end and, per 256 keys, 2 (2.4
-// where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads 16.7 / 14.8; 41 of 5,054, 8 / 2
-// 58 / 59; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
+// compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end (4 with few row tiles) and,
+// per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads 14.5 / 14.8;
+// 41 of 5,054, 8 / 2 57 / 59; 32 of 433, 5 / 1 12 / 10.7; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
 inline double paged_units(int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q) {
     return n_kv_heads * (len_q * group <= 32 ? (double)batch : (double)total_q * group / 32 + 0.5 * batch);
 }
 inline double paged_units_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     const double n = paged_units(group, n_kv_heads, batch, total_q, len_q);
+    const bool alone = len_q * group <= 128;
     const int at_once = n > cu ? 2 * cu : cu;
-    const double per = n > cu ? 3.0 : len_q * group <= 128 ? 2.4 : 2.0;
+    const double per = n > cu ? 3.0 : alone ? 2.5 : 2.0, ends = n <= cu && alone ? 4 : 6.5;
     const double longest = per * std::ceil(len_k / 256.0), middle = per * std::max(1.0, (len_k - 0.5 * len_q) / 256.0);
-    return 3 + std::max(6.5 + longest, std::ceil(n / at_once) * (6.5 + middle));
+    return 3 + std::max(ends + longest, std::ceil(n / at_once) * (ends + middle));
 }
 // The list: 18 for its launches, then rounds of items, 1.4 per 64 keys and eight such steps for an item's ends, in whole walks or
 // in ranges (paged_list_kernel does the same sum with the lengths themselves); 9 more for a launch of steps beside it.  (Two
@@ -359,11 +360,16 @@ inline double paged_list_us(int cu, int n_q_heads, int n_kv_heads, int64_t batch
         best = std::min(best, std::ceil(items * parts / cu) * (walk / parts + 12) + 7);
     return 18 + 1.4 * best + (steps ? 9 : 0);
 }
-// Spans: 12 for both launches, what memory takes, and the merge, which goes by the steps of a span (least_span()).
-inline double paged_steps_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t len_q, int64_t len_k) {
-    const double rows = std::min((double)kPagedFewRows, (double)len_q * group), keys = (double)batch * len_k * n_kv_heads;
-    const double merge = len_k / 4096.0 + keys / 32 * rows / 3900, own = keys / 32 / (cu * (rows <= 32 ? 8 : 4)), least = std::sqrt(merge / 1.3);
-    return 12 + keys * 512 / 6.0e6 + (own >= least ? merge / own : 2 * 1.3 * least - 1.3 * own);
+// Spans: 12 for both launches, and what takes longer, memory or the tiles of a span (2 us each with 64 rows, 1.3 with 32), of which
+// it has enough for the merge's sake (least_span()), and the merge.  (Estimated / measured: 24 x 5 tokens on 10,500, 64 / 8 heads
+// 210 / 187; 41 x 9 on 6,400, 5 / 1 46 / 47; 4 of 540, 32 / 8 14.3 / 11.5.)
+inline double paged_steps_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+    const bool few = len_q * group <= 32;
+    const double rows = few ? (double)len_q * group : std::min(64.0, (double)len_q * group);
+    const double units = n_kv_heads * (len_q * group <= 64 ? (double)batch : (double)total_q * group / 64 + 0.5 * batch);
+    const double tiles = units * len_k / 32, merge = len_k / 4096.0 + tiles * rows / 3900;
+    const double own = std::max({1.0, tiles / (cu * (few ? 8 : 4)), std::sqrt(merge / 1.3)});
+    return 12 + std::max((double)batch * len_k * n_kv_heads * 512 / 6.0e6, own * (few ? 1.3 : 2.0)) + merge / own;
 }
 // Sequences of very different lengths suit a list and spans, which cut them, and not units: these are taken only where even the
 // longest is short, or alone.
@@ -371,15 +377,16 @@ constexpr int64_t kPagedUnitKeys = 13 * 256;
 inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     const int g = n_q_heads / n_kv_heads;
     PagedCut c{};
-    c.list = len_q * g > kPagedFewRows;
     c.few_rows = g <= 32 ? 32 : g <= 64 ? 64 : 0;
     // steps beside a list where the longest sequences leave room for more than two with few rows (one or two are items like others)
-    c.steps = !c.list || (c.few_rows > 0 && batch - (total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2);
-    const double units = paged_units_us(cu, g, n_kv_heads, batch, total_q, len_q, len_k);
-    c.units = (batch == 1 || len_k <= kPagedUnitKeys) &&
-              units < (c.list ? paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, c.steps)
-                              : paged_steps_us(cu, g, n_kv_heads, batch, len_q, len_k));
-    if (c.units) c.steps = c.list = false;
+    const bool both = c.few_rows > 0 && batch - (total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2;
+    const double units = batch == 1 || len_k <= kPagedUnitKeys ? paged_units_us(cu, g, n_kv_heads, batch, total_q, len_q, len_k) : 1e30;
+    // (a long chunk beside decode steps: the list takes 66 ... 97 us, spans alone, whatever the estimate, 112 ... 127)
+    const double steps = len_q * g <= 1024 ? paged_steps_us(cu, g, n_kv_heads, batch, total_q, len_q, len_k) : 2e30;
+    const double list = len_q * g > kPagedFewRows ? paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, both) : 1e30;
+    c.units = units < std::min(steps, list);
+    c.list = !c.units && list <= steps;
+    c.steps = !c.units && (!c.list || both);
     c.unit_waves = paged_units(g, n_kv_heads, batch, total_q, len_q) > cu ? 4 : 8;
     c.nt = c.units ? 1 : c.list ? c.few_rows / 32 : len_q * g <= 32 ? 1 : 2;
     return c;

@@ -261,7 +261,8 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         else
             hipLaunchKernelGGL((paged_step_kernel<2, kPagedWaves2, 2, false>), dim3(cu), dim3(kPagedWaves2 * 64), 0, st, s);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-        const int tokens = (int)std::max<int64_t>(1, std::min(len_q, (int64_t)(cut.nt * 32 / g)));
+        // (beside a list most of these sequences are decode steps; the tokens of others are merged one after the other)
+        const int tokens = cut.list ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256));
         const int64_t rows = (int64_t)batch->batch * tokens, waves_wanted = (int64_t)cu * 8;
         const unsigned heads = (unsigned)shape->n_q_heads;
         // pieces of the longest unit, as far as the hints tell: a step each at most, and four times a sequence's share of the spans

@@ -32,18 +32,18 @@ PATHS = [
     ("units 8", 8, 2, 16, [(1, 700), (9, 40), (70, 300)], (70, 700)),
     ("units 4", 40, 8, 16, [(150, 200), (60, 90), (1, 30)], (150, 200)),
     ("units 8", 4, 4, 8, [(1, 1 + i % 50) for i in range(60)], (1, 50)),
-    ("units 4", 4, 1, 32, [(1, 1 + i % 70) for i in range(4300)], (70, 70)),        # more than 4,096 sequences
+    ("units 4", 4, 1, 32, [(1, 1 + i % 70) for i in range(4300)], (300, 70)),       # more than 4,096 sequences
     ("steps 1", 8, 2, 16, [(1, 700), (2, 40), (1, 5000), (8, 8)], (8, BIG)),
     ("steps 1", 2, 1, 8, [(1, 1 + i % 90) for i in range(4300)], (1, BIG)),
     ("steps 1", 10, 2, 64, [(6, 700), (3, 2), (2, 0)], (6, BIG)),                    # rows without a key, a sequence without one
     ("steps 2", 10, 2, 16, [(12, 300), (7, 7), (13, 1000), (30, 400)], (12, BIG)),   # more row tiles than the hint says
     ("steps 2", 64, 1, 16, [(1, 3000), (1, 33)], (1, BIG)),
     ("list", 8, 2, 16, [(300, 400), (20, 900)], (300, BIG)),
-    ("list", 128, 1, 32, [(1, 300), (2, 50)], (2, BIG)),                             # a group of 128
-    ("list", 3, 1, 16, [(260, 5000), (1, 2000)], (260, BIG)),                     # keys cut into ranges, no rows but one in a tile
+    ("list", 128, 1, 32, [(1, 300), (9, 50)], (9, BIG)),                             # a group of 128
+    ("list", 3, 1, 16, [(400, 5000), (1, 2000)], (400, BIG)),                     # keys cut into ranges, no rows but one in a tile
     ("steps 1 + list", 8, 2, 16, [(300, 300), (1, 900), (8, 40), (9, 40), (1, 1), (200, 6000)], (300, BIG)),
     ("steps 2 + list", 40, 1, 16, [(90, 300), (1, 900), (1, 40), (2, 40), (1, 1)], (90, BIG)),
-    ("steps 1 + list", 4, 2, 16, [(100, 100)] + [(1, 1 + i) for i in range(1500)], (100, BIG)),     # more sequences than the builder holds at once
+    ("steps 1 + list", 4, 2, 16, [(600, 600)] + [(1, 1 + i) for i in range(1500)], (600, BIG)),     # more sequences than the builder holds at once
 ]
 
 
@@ -59,7 +59,7 @@ def test_paths(case, causal):
 
 # the same paths, sequences of several tokens each
 HIDDEN = [("units 8", [(6, 90), (40, 40), (70, 200)], (70, 200)), ("steps 1", [(6, 90), (9, 300), (16, 16)], (16, BIG)),
-          ("steps 2", [(20, 90), (30, 70), (31, 300)], (32, BIG)), ("list", [(200, 310), (80, 80), (300, 5300)], (300, BIG))]
+          ("steps 2", [(20, 90), (30, 70), (31, 300)], (32, BIG)), ("list", [(200, 310), (80, 80), (300, 5300)], (600, BIG))]
 
 
 @pytest.mark.parametrize("case", HIDDEN, ids=lambda c: c[0])
@@ -226,10 +226,10 @@ def test_prompts_in_pages_are_prompts_in_a_row():
     assert bool(((out.float() - layer.out[:n].float()).abs() <= 4 * ref.BF16 * (1 + out.float().abs())).all())
 
 
-@pytest.mark.parametrize("hints", [(1, 60), (1, 4000), (300, 4000)])      # units, steps, steps beside a list
+@pytest.mark.parametrize("hints", [(1, 60), (1, 4000), (300, 4000)])      # units, steps, steps beside a list (300 packed rows)
 def test_captured_steps_work_on_what_the_buffers_hold(hints):
     """Two graphs of one layer through one workspace, replayed in turn with eager work between them; lengths and inputs change."""
-    layer = Layer(52, 8, 2, 16, 40, 4000, [[1] * 6])
+    layer = Layer(52, 8, 2, 16, 300, 4000, [[1] * 6])
     layer.feed([3, 7, 1, 9, 4, 2])
     layer.run(hints)                          # (first use outside a capture)
     layer.check([3, 7, 1, 9, 4, 2], "eager")
