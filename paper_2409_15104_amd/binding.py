@@ -517,6 +517,8 @@ def _rows(t, name: str, index: int) -> int:
         if sizes[0] == 0:
             return 0
         raise ValueError("the heads of a token must be contiguous in %s" % name)
+    if strides[0] < 128 * sizes[1] and sizes[0] > 0:
+        raise ValueError("the tokens of %s overlap" % name)
     return strides[0]
 
 
@@ -534,7 +536,7 @@ def _paged_batch(block_table, cu_seqlens_q, seqlens_k, total_q, max_len_q, max_l
     if len(sizes) != 2 or sizes[0] != batch or cu_seqlens_q.numel() != batch + 1:
         raise ValueError("block_table must be [batch, pages], cu_seqlens_q [batch + 1] and seqlens_k [batch]")
     return _BATCH_FORMAT(_on(cu_seqlens_q, _I32, "cu_seqlens_q", index), _on(seqlens_k, _I32, "seqlens_k", index),
-                         _on(block_table, _I32, "block_table", index), batch, sizes[1], total_q, max_len_q, max_len_k)
+                         _on(block_table, _I32, "block_table", index), batch, sizes[1], total_q, int(max_len_q), int(max_len_k))
 
 
 @functools.lru_cache(maxsize=256)
@@ -580,7 +582,7 @@ def pec_qk_norm_rope(q, k, norm_rope: NormRope, positions=None, pos0: int = 0, q
     at = _on(positions, _I32, "positions", index, (tokens,)) if positions is not None else None
     hkv = given.shape[1] if k is None else k.shape[1]      # (of queries or keys alone: as many of the other)
     shp = _shape_ref(given.shape[1], hkv, _BF16, 0.0, 0)
-    _call(lib().pec_qk_norm_rope, "pec_qk_norm_rope", index, stream, shp, norm_rope.ref, q_at, q_stride, k_at, k_stride, at, pos0,
+    _call(lib().pec_qk_norm_rope, "pec_qk_norm_rope", index, stream, shp, norm_rope.ref, q_at, q_stride, k_at, k_stride, at, int(pos0),
           tokens, qo_at, ko_at)
     return q_out, k_out
 
@@ -633,10 +635,12 @@ def pec_attn_paged(q, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, m
         lse = torch.empty((hq, total), dtype=_F32, device=q.device)
     out_at, lse_at = _on(out, out_dtype, "out", index, sizes), _on(lse, _F32, "lse", index, (hq, total))
     batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, total, max_len_q, max_len_k, index)
-    shp = _shape_ref(hq, cache.n_kv_heads, out_dtype, float(scale), flags)
+    shp = _shape_ref(hq, cache.n_kv_heads, out_dtype, float(scale), int(flags))
     if workspace is None:
         n = int(lib().pec_paged_workspace_bytes(shp, seqlens_k.numel(), total))
         workspace = torch.empty(max(16, n), dtype=_U8, device=q.device)
+        if stream is not None:      # (not handed out again while that stream still works with it)
+            workspace.record_stream(stream)
     _call(lib().pec_attn_paged, "pec_attn_paged", index, stream, shp, cache.ref, batch, q.data_ptr(), q_stride, 1 if causal else 0, out_at,
           lse_at, _on(workspace, _U8, "workspace", index), workspace.numel())
     return out, lse

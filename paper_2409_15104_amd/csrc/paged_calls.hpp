@@ -137,7 +137,7 @@ int pec_qk_norm_rope(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
     if (tokens > kMaxRows) return PEC_ERR_UNSUPPORTED;
     if (tokens == 0) return PEC_OK;
     if ((!q && !k) || (q && !q_out) || (k && !k_out)) return PEC_ERR_INVALID_ARGUMENT;
-    if (!positions && p.rotary > 0 && pos0 + tokens > p.n_positions) return PEC_ERR_INVALID_ARGUMENT;
+    if (!positions && p.rotary > 0 && pos0 > p.n_positions - tokens) return PEC_ERR_INVALID_ARGUMENT;
     p.q_stride = token_stride(q_stride, shape->n_q_heads);
     p.k_stride = token_stride(k_stride, shape->n_kv_heads);
     if ((q && p.q_stride < 0) || (k && p.k_stride < 0)) return PEC_ERR_INVALID_ARGUMENT;

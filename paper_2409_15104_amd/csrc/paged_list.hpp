@@ -87,8 +87,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         const int parts = wave < 8 ? wave + 1 : wave == 8 ? 10 : wave == 9 ? 12 : wave == 10 ? 16 : wave == 11 ? 20
                         : wave == 12 ? 24 : wave == 13 ? 32 : wave == 14 ? 48 : 64;
         const int steps = max(16, (whole + parts - 1) / parts), range = wave == 0 || p.slot_capacity == 0 ? 0x40000000 : steps * kBN;
-        int64_t all_keys = 0;
-        int items = 0, uncut = 0, tiles = 0;
+        int64_t all_keys = 0, items = 0, uncut = 0, tiles = 0;
         // a lane per sequence, or, of up to eight sequences, eight lanes that share its ranges
         const int per = bt.batch <= 8 ? 8 : 1, sub = lane % per;
         for (int b = lane / per; b < bt.batch; b += 64 / per) {
@@ -108,8 +107,13 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
             tiles += __shfl_xor(tiles, off);
             keys += __shfl_xor(keys, off);
         }
+        // (offsets that fall make sequences overlap, and then there may be more tiles than the list has room for: no item at all)
+        if (tiles > p.capacity - p.slot_capacity) {
+            if (tid == 0) p.counters[0] = p.counters[2] = 0;
+            return;
+        }
         if (lane == 0) {
-            const int cut = items - uncut;      // items with partial results
+            const int64_t cut = items - uncut;      // items with partial results
             const float units = (float)p.units, work = (keys / kBN + 0.5f * tiles + 8.f * items + 4.f * cut) * units / p.cu;
             const float one = (float)min(whole, range / kBN) + 8.f + (cut > 0 ? 4.f : 0.f);
             const float rounds = ceilf(items * units / p.cu);
@@ -170,8 +174,8 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
                 int slot0 = -1;
                 if (n_ranges > 1) {
                     slot0 = atomicAdd(&n_slots, n_ranges);
-                    if (slot0 + n_ranges > p.slot_capacity) continue;      // (never, unless the offsets change under the launch)
-                    p.splits[atomicAdd(&n_split, 1)] = PagedSplit{c0 + i, tile, slot0, n_ranges};
+                    if (slot0 + n_ranges > p.slot_capacity) slot0 = -1;      // (never, unless the offsets change under the launch)
+                    else p.splits[atomicAdd(&n_split, 1)] = PagedSplit{c0 + i, tile, slot0, n_ranges};
                 }
                 int pos = pos0[i] + t.n - 1 - tile;
                 for (int r = 0; r < n_ranges; ++r) {

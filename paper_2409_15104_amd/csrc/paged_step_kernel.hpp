@@ -30,6 +30,10 @@ constexpr int kStepTile = 32;
 constexpr int kStepTileBytes = kStepTile * kRowBytes;
 constexpr int kPagedChunks = 1024;                     // sequences are added up 64 at a time: up to 65,536 of them
 
+// Sums that stop at kTooMany: the host refuses calls of so many steps, but offsets that fall can make sequences overlap, and
+// sums of overlapping ones anything.
+constexpr int kTooMany = 0x7fffffff;
+__device__ __forceinline__ int add_up(int x, int y) { return (int)min((uint32_t)x + (uint32_t)y, (uint32_t)kTooMany); }
 
 // How a call's sequences are cut: R = 2^log_r rows a unit; a sequence has less than 2^31 rows.
 struct StepCut {
@@ -49,7 +53,7 @@ struct StepCut {
     __device__ __forceinline__ int all_tiles(const PagedSeq& s) const {
         const int n = row_tiles(s);
         int sum = 0;
-        for (int rt = 0; rt < n; ++rt) sum += tiles(s, rt);
+        for (int rt = 0; rt < n; ++rt) sum = add_up(sum, tiles(s, rt));
         return sum;
     }
 };
@@ -68,7 +72,7 @@ __device__ __forceinline__ int wave_prefix(int x) {      // inclusive
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
+        if (lane >= d) x = add_up(x, y);
     }
     return x;
 }
@@ -124,7 +128,7 @@ struct PagedLine {
         }
         __syncthreads();
         int sum = 0;
-        for (int c = lane; c < n_chunks; c += 64) sum += chunk_sum[c];
+        for (int c = lane; c < n_chunks; c += 64) sum = add_up(sum, chunk_sum[c]);
         total = __builtin_amdgcn_readlane(wave_prefix(sum), 63);
     }
     __device__ __forceinline__ PagedSeq seq(int i) const {       // uniform
@@ -196,13 +200,13 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
     if (!SHARED && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
         for (int c = wave, ahead = 0, at = 0; c < line.n_chunks; c += WAVES) {
-            for (; at < c; ++at) ahead += chunk_sum[at];
+            for (; at < c; ++at) ahead = add_up(ahead, chunk_sum[at]);
             const int mine = length(line.load(64 * c + lane)), all = wave_prefix(mine);
-            if (64 * c + lane < bt.batch) p.prefix[64 * c + lane] = ahead + all - mine;
+            if (64 * c + lane < bt.batch) p.prefix[64 * c + lane] = add_up(ahead, all) - mine;
         }
-        if (threadIdx.x == 0) p.prefix[bt.batch] = line.total;
+        if (threadIdx.x == 0) p.prefix[bt.batch] = line.total == kTooMany ? 0 : line.total;
     }
-    if (line.total == 0) return;
+    if (line.total == 0 || line.total == kTooMany) return;
     int least = 1;
     if constexpr (!SHARED) {
         int longest = line.total / 64;       // (of more than 64 sequences: that many alike)
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     int at, left, kvh, w = 0;               // place on the line, tiles to work on
     if constexpr (SHARED) {
         const WorkOrder order(line.total, 1, p.a.n_kv_heads);
-        if ((blockIdx.x >> 3) >= order.count) return;
+        if ((blockIdx.x >> 3) >= order.count || order.total > gridDim.x) return;      // (more units than the rows make: as above)
         const int64_t unit = order.unit(blockIdx.x & 7, blockIdx.x >> 3);
         if (unit < 0) return;
         kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
@@ -257,8 +261,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
         int seq = u.seq, rt = u.rt + 1;
         while (rt >= cut.row_tiles(s)) {
             rt = 0;
-            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch)
+            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch: what is left has no rows and no keys)
                 seq = 0;
+                s = PagedSeq{0, 0, 0};
                 break;
             }
             s = line.seq(seq);

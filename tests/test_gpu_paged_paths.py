@@ -250,6 +250,38 @@ def test_captured_steps_work_on_what_the_buffers_hold(hints):
             layer.check([1] * 6, "eager between replays")
 
 
+@pytest.mark.parametrize("case", HIDDEN, ids=lambda c: c[0])
+def test_a_stream_given_keeps_its_workspace(case):
+    """What is allocated behind the call on the current stream is not the workspace that the other stream works with."""
+    _, seqs, hints = case
+    b = ref.Batch(35, 4, 2, 16, seqs, table_extra=BIG // 16)
+    alone = attend(b, hints)
+    kc, vc, bt, cu, lk = b.to(DEV)
+    cache, q, side = pec.PagedCache(kc, vc), b.q.to(DEV), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    n = pec.pec_paged_workspace_bytes(4, 2, len(seqs), b.total)
+    out, lse = torch.zeros_like(q), torch.zeros(4, b.total, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        pec.pec_attn_paged(q, cache, bt, cu, lk, *hints, out=out, lse=lse, stream=side)
+        torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        assert torch.equal(out, alone[0]) and torch.equal(lse, alone[1])
+
+
+@pytest.mark.parametrize("hints", [(1, 60), (16, BIG), (32, BIG), (300, BIG)])
+def test_sequences_that_overlap(hints):
+    """Offsets that fall again and again, more rows in all than there are packed ones: some result, the rows of no sequence left
+    alone, and the next call as ever."""
+    seqs = [(300, 400)] + [(0, 60)] * 39
+    b = ref.Batch(36, 4, 2, 16, seqs, spare_rows=3, table_extra=BIG // 16)
+    right = b.cu
+    b.cu = torch.tensor([0, 300] * 20 + [300], dtype=torch.int32)
+    attend(b, hints, workspace=torch.full((pec.pec_paged_workspace_bytes(4, 2, 40, b.total),), 255, dtype=torch.uint8, device=DEV))
+    b.cu = right
+    ref.assert_attention(*attend(b, hints), ref.attention(b), str(hints))
+
+
 def test_append_in_place():
     """q_out may be a packed q."""
     b = ref.Batch(53, 4, 2, 16, [(5, 30), (1, 8)])

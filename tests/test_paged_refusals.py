@@ -104,6 +104,28 @@ def test_attention_refusals():
     assert attn(s=shape(scale=-1.0)) == INVALID and attn(s=shape(dtype=9)) == UNSUPPORTED
 
 
+def test_head_rows_of_the_binding():
+    z = torch.zeros(6, 5, 128, dtype=torch.bfloat16)
+    assert pec._rows(z, "q", -1) == 640 and pec._rows(z[:, :2], "q", -1) == 640 and pec._rows(z[::2], "q", -1) == 1280
+    assert pec._rows(z[:1, 1:2], "q", -1) == 0 and pec._rows(z[:0], "q", -1) == 0
+    for bad in (z[:1].expand(6, 5, 128), z.transpose(0, 1), z.float(), z[:, ::2], z[..., :64], z[0]):
+        with pytest.raises(ValueError):
+            pec._rows(bad, "q", -1)
+    with pytest.raises(ValueError):
+        pec._rows(z, "q", 0)
+
+
+def test_calls_that_no_count_holds():
+    """More sequences than are added up, more rows or tile steps than have a number, more KV heads than wavefronts."""
+    big = 1 << 60
+    assert attn(b=batch(batch=65537, total_q=65537), nbytes=big) == UNSUPPORTED
+    assert attn(s=shape(64, 1), b=batch(total_q=1 << 26), nbytes=big) == UNSUPPORTED
+    assert attn(s=shape(2, 2), b=batch(batch=60000, total_q=60000, table_len=1 << 24, max_len_q=1), nbytes=big) == UNSUPPORTED
+    wide = shape(2100, 2100)
+    c = cache(row_stride=2100 * 128, page_stride=16 * 2100 * 128)
+    assert attn(s=wide, c=c, b=batch(batch=2, total_q=2, max_len_q=1, table_len=1 << 10), nbytes=big) == UNSUPPORTED
+
+
 def test_workspace_never_falls():
     for hq, hkv in ((8, 2), (32, 8), (40, 40)):
         for b, t in ((1, 1), (4, 4), (64, 64), (64, 5000), (500, 100000)):
