@@ -61,7 +61,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
     };
     __shared__ Seq seqs[kPagedListSeqs];
     __shared__ int32_t bucket[kPagedListBuckets];
-    __shared__ int32_t red[16], n_slots, n_split, range_lds;
+    __shared__ int32_t red[16], n_slots, n_split;
     __shared__ float cost[16];
     __shared__ int32_t cand[16];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -69,10 +69,18 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
     if (tid == 0) n_slots = n_split = 0;
     if (tid >= 8 && tid < 16) p.counters[tid] = 0;
 
-    // ---- the longest walk, then the estimates
+    // ---- the longest walk, then the estimates.  Up to 1,024 sequences are read once and stay in LDS.
+    const bool held = bt.batch <= kPagedListSeqs;
+    auto seq_at = [&](int b) { return held ? seqs[b].s : paged_seq(bt, b); };
+    // Lanes that share a sequence: of up to 64, as many as a wavefront has for each; above, one.
+    int log_per = 0;
+    while (bt.batch << log_per << 1 <= 64) ++log_per;
+    const int per = 1 << log_per, sub = lane & (per - 1), mine = lane >> log_per;
     int longest = 0;
     for (int b = tid; b < bt.batch; b += 1024) {
-        const PagedTiles t(paged_seq(bt, b), p);
+        const PagedSeq s = paged_seq(bt, b);
+        if (held) seqs[b].s = s;
+        const PagedTiles t(s, p);
         if (t.n > 0) longest = max(longest, t.keys(t.n - 1));
     }
 #pragma unroll
@@ -87,19 +95,16 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         const int parts = wave < 8 ? wave + 1 : wave == 8 ? 10 : wave == 9 ? 12 : wave == 10 ? 16 : wave == 11 ? 20
                         : wave == 12 ? 24 : wave == 13 ? 32 : wave == 14 ? 48 : 64;
         const int steps = max(16, (whole + parts - 1) / parts), range = wave == 0 || p.slot_capacity == 0 ? 0x40000000 : steps * kBN;
-        int64_t all_keys = 0, items = 0, uncut = 0, tiles = 0;
-        // a lane per sequence, or, of up to eight sequences, eight lanes that share its ranges
-        const int per = bt.batch <= 8 ? 8 : 1, sub = lane % per;
-        for (int b = lane / per; b < bt.batch; b += 64 / per) {
-            const PagedTiles t(paged_seq(bt, b), p);
+        float items = 0.f, uncut = 0.f, tiles = 0.f, keys = 0.f;      // (whole numbers, exact up to 2^24 of them)
+        for (int b = mine; b < bt.batch; b += 64 >> log_per) {
+            const PagedTiles t(seq_at(b), p);
             if (t.n == 0) continue;
-            items += t.items(range, sub, per);
+            items += (float)t.items(range, sub, per);
             if (sub != 0) continue;
-            uncut += t.first_beyond(range);
-            tiles += t.n;
-            all_keys += ((int64_t)t.keys(0) + t.keys(t.n - 1)) * t.n / 2;
+            uncut += (float)t.first_beyond(range);
+            tiles += (float)t.n;
+            keys += ((float)t.keys(0) + (float)t.keys(t.n - 1)) * (float)t.n * 0.5f;
         }
-        float keys = (float)all_keys;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) {
             items += __shfl_xor(items, off);
@@ -108,38 +113,97 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
             keys += __shfl_xor(keys, off);
         }
         // (offsets that fall make sequences overlap, and then there may be more tiles than the list has room for: no item at all)
-        if (tiles > p.capacity - p.slot_capacity) {
+        if (tiles > 1.001f * (p.capacity - p.slot_capacity)) {
             if (tid == 0) p.counters[0] = p.counters[2] = 0;
             return;
         }
         if (lane == 0) {
-            const int64_t cut = items - uncut;      // items with partial results
+            const float cut = items - uncut;      // items with partial results
             const float units = (float)p.units, work = (keys / kBN + 0.5f * tiles + 8.f * items + 4.f * cut) * units / p.cu;
-            const float one = (float)min(whole, range / kBN) + 8.f + (cut > 0 ? 4.f : 0.f);
+            const float one = (float)min(whole, range / kBN) + 8.f + (cut > 0.f ? 4.f : 0.f);
             const float rounds = ceilf(items * units / p.cu);
-            float c = fmaxf(one, fminf(rounds * one, work + 0.5f * one)) + (cut > 0 ? 8.f : 0.f);
+            float c = fmaxf(one, fminf(rounds * one, work + 0.5f * one)) + (cut > 0.f ? 8.f : 0.f);
             if (cut > p.slot_capacity) c = INFINITY;
             cost[wave] = c;
             cand[wave] = range;
         }
     }
     __syncthreads();
-    if (tid == 0) {
-        int best = 0;
-        for (int i = 1; i < 16; ++i)
-            if (cost[i] < cost[best]) best = i;
-        range_lds = cand[best];
+    int range;
+    {
+        float least = cost[lane & 15];
+        int best = lane & 15;
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) {
+            const float other = __shfl_xor(least, off);
+            const int its = __shfl_xor(best, off);
+            if (other < least || (other == least && its < best)) {
+                least = other;
+                best = its;
+            }
+        }
+        range = cand[__builtin_amdgcn_readfirstlane(best)];
     }
+
+    // ---- items of sequence `b`, from place `pos0` of the list on: range by range, the last tile first
+    auto place = [&](int b, const PagedSeq& sq, int pos0) {
+        const PagedTiles t(sq, p);
+        for (int tile = lane; tile < t.n; tile += 64) {
+            const int keys = t.keys(tile), n_ranges = max(1, (int)(((int64_t)keys + range - 1) / range));
+            int slot0 = -1;
+            if (n_ranges > 1) {
+                slot0 = atomicAdd(&n_slots, n_ranges);
+                if (slot0 + n_ranges > p.slot_capacity) slot0 = -1;      // (never, unless the offsets change under the launch)
+                else p.splits[atomicAdd(&n_split, 1)] = PagedSplit{b, tile, slot0, n_ranges};
+            }
+            int pos = pos0 + t.n - 1 - tile;
+            for (int r = 0; r < n_ranges; ++r) {
+                if (r > 0) pos += t.n - (r == 1 ? 0 : t.first_beyond((r - 1) * range));
+                const int key0 = r * range;
+                if ((uint32_t)pos < (uint32_t)p.capacity)
+                    p.work[pos] = WorkItem{sq.q0, sq.len_q, b, sq.len_k, tile, slot0 < 0 ? -1 : slot0 + r,
+                                           {n_ranges > 1 ? key0 : 0, n_ranges > 1 ? min(keys, key0 + range) : keys}};
+            }
+        }
+    };
+
+    // ---- sequences by their longest walk.  Up to 64: a wavefront adds up for itself what is ahead of its ones, without a barrier.
+    if (bt.batch <= 64) {
+        int walk = -1, n_items = 0;
+        if (mine < bt.batch) {
+            const PagedTiles t(seqs[mine].s, p);
+            if (t.n > 0) {
+                walk = t.keys(t.n - 1);
+                n_items = t.items(range, sub, per);
+            }
+        }
+        for (int off = per >> 1; off > 0; off >>= 1) n_items += __shfl_xor(n_items, off);
+        auto sum = [&](int x) {
+            for (int off = 32; off >= per; off >>= 1) x += __shfl_xor(x, off);
+            return x;
+        };
+        if (wave == 15) {       // (the least to do otherwise)
+            const int total = sum(n_items);
+            if (lane == 0) p.counters[0] = min(total, p.capacity);
+        }
+        for (int b = wave; b < bt.batch; b += 16) {
+            if (__builtin_amdgcn_readlane(n_items, b << log_per) == 0) continue;
+            const int its = __builtin_amdgcn_readlane(walk, b << log_per);
+            place(b, seqs[b].s, sum(walk > its || (walk == its && mine < b) ? n_items : 0));
+        }
+        __syncthreads();
+        if (tid == 0) p.counters[2] = n_split;
+        return;
+    }
+
+    // ---- of more, by buckets of alike ones
     for (int t = tid; t < kPagedListBuckets; t += 1024) bucket[t] = 0;
     __syncthreads();
-    const int range = range_lds;
-
-    // ---- sequences by their longest walk, the items of a sequence together: range by range, the last tile first
     auto load_seq = [&](int c0) {
         const int b = c0 + tid;
         if (b >= bt.batch) return;
         Seq q;
-        q.s = paged_seq(bt, b);
+        q.s = held ? seqs[tid].s : paged_seq(bt, b);
         const PagedTiles t(q.s, p);
         q.n_items = t.n > 0 ? t.items(range, 0, 1) : 0;
         seqs[tid] = q;
@@ -166,26 +230,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         __syncthreads();
         const int n = min(bt.batch - c0, kPagedListSeqs);
         for (int i = wave; i < n; i += 16) {
-            const Seq q = seqs[i];
-            if (q.n_items == 0) continue;
-            const PagedTiles t(q.s, p);
-            for (int tile = lane; tile < t.n; tile += 64) {
-                const int keys = t.keys(tile), n_ranges = max(1, (int)(((int64_t)keys + range - 1) / range));
-                int slot0 = -1;
-                if (n_ranges > 1) {
-                    slot0 = atomicAdd(&n_slots, n_ranges);
-                    if (slot0 + n_ranges > p.slot_capacity) slot0 = -1;      // (never, unless the offsets change under the launch)
-                    else p.splits[atomicAdd(&n_split, 1)] = PagedSplit{c0 + i, tile, slot0, n_ranges};
-                }
-                int pos = pos0[i] + t.n - 1 - tile;
-                for (int r = 0; r < n_ranges; ++r) {
-                    if (r > 0) pos += t.n - (r == 1 ? 0 : t.first_beyond((r - 1) * range));
-                    const int key0 = r * range;
-                    if ((uint32_t)pos < (uint32_t)p.capacity)
-                        p.work[pos] = WorkItem{q.s.q0, q.s.len_q, c0 + i, q.s.len_k, tile, slot0 < 0 ? -1 : slot0 + r,
-                                               {n_ranges > 1 ? key0 : 0, n_ranges > 1 ? min(keys, key0 + range) : keys}};
-                }
-            }
+            if (seqs[i].n_items > 0) place(c0 + i, seqs[i].s, pos0[i]);
         }
     }
     __syncthreads();
