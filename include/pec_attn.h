@@ -385,7 +385,10 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
  *   q [total_q, Hq, 128] with q_stride elements from token to token (0 = packed); out [total_q, Hq, 128] in shape->out_dtype,
  *   lse [Hq, total_q].  Rows without a visible key get out = 0, lse = -inf; a row whose weights are NaN gets NaN in both.
  *   workspace: pec_paged_workspace_bytes() bytes, 16-byte aligned, whatever they hold; calls that may run at the same time need
- *   one each.
+ *   one each.  Neither out, lse nor the workspace may overlap q or the cache.
+ * Limits (PEC_ERR_UNSUPPORTED beyond them): 65,536 sequences; total_q * (Hq / Hkv) < 2^31 - 64 query rows per KV head; 1,024 KV
+ * heads; and, counted with the longest sequence that block_table has room for, 2^31 - 1 steps of 32 keys for all sequences' blocks
+ * of 32 rows (65,536 sequences of up to 32 rows: half a million keys each).
  * PEC_FLAG_SIMPLE_KERNEL runs the plain kernel (fp32 weights, a wavefront per row; needs no workspace).
  */
 int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,

@@ -336,8 +336,9 @@ struct PagedCut {
 };
 // Units: rounds of workgroups of eight wavefronts, or, where there are more of them than compute units, of four with two to a
 // compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end (4 with few row tiles) and,
-// per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads 14.5 / 14.8;
-// 41 of 5,054, 8 / 2 57 / 59; 32 of 433, 5 / 1 12 / 10.7; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
+// per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads
+// 14.5 / 14.8; 41 of 5,054, 8 / 2 57 / 59; 32 of 433, 5 / 1 12 / 10.7; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48;
+// 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
 inline double paged_units(int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q) {
     return n_kv_heads * (len_q * group <= 32 ? (double)batch : (double)total_q * group / 32 + 0.5 * batch);
 }

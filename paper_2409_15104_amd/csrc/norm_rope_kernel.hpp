@@ -69,7 +69,8 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
         if (i >= end) return x;
         const int kind = kind_of(i), head = 4 * (i - (kind == Q ? 0 : kind == K ? q_quads : q_quads + k_quads)) + sub;
         const __bf16* const row = kind == Q ? p.q + token * p.q_stride : kind == K ? p.k + token * p.k_stride : p.v + token * p.v_stride;
-        if (head < (kind == Q ? p.n_q_heads : p.n_kv_heads)) x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + head * kHeadDim + 8 * c));
+        if (head < (kind == Q ? p.n_q_heads : p.n_kv_heads))
+            x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + head * kHeadDim + 8 * c));
         return x;
     };
     u32x4 ahead[kNormRopeAhead];

@@ -15,7 +15,13 @@
 // its address from scalar registers.  The page numbers of the next tile are scalar loads a tile ahead: they count against
 // lgkmcnt, which the LDS reads bring to zero anyway, and not against vmcnt, by which the tiles are waited for.
 //
-// NT = 1: eight wavefronts per workgroup, one stage.  NT = 2 (up to 64 rows): four wavefronts with 512 registers each, two stages.
+// NT = 1: eight wavefronts per workgroup, one stage.  NT = 2 (up to 64 rows): four wavefronts with 512 registers each, two stages
+// (eight with one stage, and 256 registers, spill: 318 us in the place of 187 for the 24 sequences below).
+//
+// What bounds it, spans with their merge: memory, 4 sequences of 107,500 tokens, 64 / 8 heads (1.76 GB) 275 us, 6.4 TB/s, as a
+// streaming read; 64 of 27 ... 7,400, 32 / 8 (450 MB) 83 us, of which the merge takes 6; 24 x 5 drafted tokens behind 10,350,
+// 64 / 8, rows of two fragments (1.02 GB) 187 us, 5.7 TB/s while the spans run.  4 of 540, 32 / 8 (9 MB) 11.5 us: launches, three
+// trips to memory each, and three tiles per wavefront.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -322,7 +328,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     auto look_up = [&]() {
         const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)req.seq * bt.table_len);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) number[i] = req.keys == 0 ? 0 : (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
+        for (int i = 0; i < 4; ++i)
+            number[i] = req.keys == 0 ? 0 : (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
     };
     auto locate = [&]() {
 #pragma unroll
@@ -505,7 +512,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
                         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                             for (int b = 0; b < 4; ++b) {
-                                const bf16x4 x = *reinterpret_cast<const bf16x4*>(row + (v_lds_off(key, 64 * dt + 16 * b + 8 * hl) - key * kRowBytes));
+                                const int at = v_lds_off(key, 64 * dt + 16 * b + 8 * hl) - key * kRowBytes;
+                                const bf16x4 x = *reinterpret_cast<const bf16x4*>(row + at);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const float y = (float)x[i];
@@ -668,7 +676,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
     __shared__ __attribute__((aligned(16))) float red[N][kHeadDim];
     __shared__ float red_mx[N], red_den[N];
     const PagedBatch& bt = p.a.batch;
-    const int g = p.a.group, head = blockIdx.y, kvh = p.cut.group.div(head), in_group = head - kvh * g, log_r = p.cut.log_r, grp = (int)(threadIdx.x >> 5) % N, c = threadIdx.x & 31;
+    const int g = p.a.group, head = blockIdx.y, kvh = p.cut.group.div(head), in_group = head - kvh * g, log_r = p.cut.log_r;
+    const int grp = (int)(threadIdx.x >> 5) % N, c = threadIdx.x & 31;
     const int per_head = p.prefix[bt.batch], least = p.prefix[bt.batch + 1];
     constexpr int PER_GROUP = WAVES == 1 ? 4 : 1;       // rows a workgroup works on at a time
     for (int x = blockIdx.x * PER_GROUP + (WAVES == 1 ? (int)(threadIdx.x >> 6) : 0); x < bt.batch * tokens; x += gridDim.x * PER_GROUP) {
@@ -694,7 +703,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
                     l[i] = -INFINITY;
                     o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if (w + i * N <= w1) {
-                        const int64_t slot_row = ((((int64_t)(w + i * N) * p.a.n_kv_heads + kvh) * 2 + (w + i * N == w0 ? 1 : 0)) << log_r) + row;
+                        const int64_t slot = ((int64_t)(w + i * N) * p.a.n_kv_heads + kvh) * 2 + (w + i * N == w0 ? 1 : 0);
+                        const int64_t slot_row = (slot << log_r) + row;
                         l[i] = p.part_lse[slot_row];
                         o[i] = *reinterpret_cast<const f32x4*>(p.part_out + slot_row * kHeadDim + 4 * c);
                     }
@@ -730,7 +740,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
                 }
                 if (grp == 0) {
                     if (p.a.out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.a.out) + out_row + 4 * c) = acc;
-                    else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + out_row + 4 * c) = __builtin_convertvector(acc, bf16x4);
+                    else
+                        *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + out_row + 4 * c) = __builtin_convertvector(acc, bf16x4);
                     if (c == 0) p.a.lse[lse_at] = den == 0.f ? -INFINITY : ref + logf(den);
                 }
             } else {
