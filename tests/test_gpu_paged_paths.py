@@ -282,6 +282,25 @@ def test_sequences_that_overlap(hints):
     ref.assert_attention(*attend(b, hints), ref.attention(b), str(hints))
 
 
+@pytest.mark.parametrize("hints", [(1, BIG), (700, BIG)])      # steps, steps beside a list
+def test_as_many_sequences_as_there_may_be(hints):
+    """65,536 sequences of one token, appended and looked at: the result is the token's own value, the LSE its score."""
+    n, hq, hkv = 65536, 4, 2
+    g = torch.Generator().manual_seed(37)
+    k, v, q = [torch.randn(n, h, 128, generator=g).to(torch.bfloat16) for h in (hkv, hkv, hq)]
+    table = torch.full((n, BIG // 8), -1, dtype=torch.int32, device=DEV)
+    table[:, 0] = torch.randperm(n, generator=g).to(torch.int32).to(DEV)
+    cache = pec.PagedCache(*[torch.full((n, 8, hkv, 128), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2)])
+    cu, lk = torch.arange(n + 1, dtype=torch.int32, device=DEV), torch.ones(n, dtype=torch.int32, device=DEV)
+    pec.pec_paged_append(k.to(DEV), v.to(DEV), cache, table, cu, lk)
+    out, lse = pec.pec_attn_paged(q.to(DEV), cache, table, cu, lk, *hints)
+    assert torch.equal(out.cpu(), v.repeat_interleave(hq // hkv, dim=1))      # (a weight of 1 and a sum within 2^-20 of 1)
+    product = q.double() * k.repeat_interleave(hq // hkv, dim=1).double() * 128 ** -0.5
+    want = product.sum(dim=-1)
+    err = (lse.cpu().double().T - want).abs()
+    assert bool((err <= 2 * (128 * ref.F32 * product.abs().sum(dim=-1) + 2.0 ** -20) + 2.0 ** -20 * want.abs()).all())
+
+
 def test_append_in_place():
     """q_out may be a packed q."""
     b = ref.Batch(53, 4, 2, 16, [(5, 30), (1, 8)])
