@@ -332,7 +332,8 @@ typedef struct {
 } pec_paged_batch_t;
 
 /*
- * What happens to a row of 128 of a query or key head ahead of attention, in fp32 with one rounding to bf16 at the end:
+ * What happens to a row of 128 of a query or key head ahead of attention, in fp32 (a row whose squares add up to more than fp32
+ * holds has no norm) with one rounding to bf16 at the end:
  *   1. norm, if there is a weight: x * weight / sqrt(mean(x^2) + eps);
  *   2. rotation of the first rotary_dim values (R), if it is not 0: (a, b) -> (a cos - b sin, b cos + a sin) of the pairs
  *      (i, i + R/2), or (2i, 2i + 1) with interleaved != 0, i < R/2, with the angles of the token's position p:
