@@ -334,16 +334,23 @@ struct PagedCut {
     int unit_waves;          // wavefronts of a unit's workgroup
     int nt, few_rows;        // few_rows: rows up to which a sequence goes to the steps where both run
 };
-// Units: rounds of workgroups of eight wavefronts, or, where there are more of them than compute units, of four with two to a
-// compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end (4 with few row tiles) and,
-// per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 57 sequences of 565 tokens, 16 / 4 heads
-// 14.5 / 14.8; 41 of 5,054, 8 / 2 57 / 59; 32 of 433, 5 / 1 12 / 10.7; 953 new tokens, 5 / 1 17.5 / 14.7; 5,189, 1 / 1 51 / 48;
-// 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
+// Units of several to a sequence: rounds of workgroups of eight wavefronts, or, where there are more of them than compute units, of
+// four with two to a compute unit, so that one's start and end hide under the other's walk; 6.5 for a unit's start and end (4 with
+// few row tiles) and, per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 953 new tokens, 5 / 1 heads
+// 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
+// One unit per sequence and KV head, which has its keys to itself: 2.05 per 256 keys, or 7.5 a round, against memory.  (477 calls of
+// 1 ... 128 sequences on 60 ... 3,300 keys, with units and with spans: the mean estimate is off by 7 %, the choice costs 0.3 % on the
+// mean.  4 of 540, 32 / 8 heads, 10.2 as units, 11.7 as spans; of 1,000 14.9 and 12.8; 32 of 1,000 23.5 and 31.0.)
 inline double paged_units(int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q) {
     return n_kv_heads * (len_q * group <= 32 ? (double)batch : (double)total_q * group / 32 + 0.5 * batch);
 }
 inline double paged_units_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     const double n = paged_units(group, n_kv_heads, batch, total_q, len_q);
+    if (len_q * group <= 32) {
+        const double memory = (double)batch * len_k * n_kv_heads * 512 / 6.3e6;
+        return n <= cu ? 5.6 + len_q * group / 16.0 + std::hypot(2.05 * len_k / 256, memory)
+                       : 2 + std::hypot(7.5 * std::ceil(n / (2 * cu)), memory);
+    }
     const bool alone = len_q * group <= 128;
     const int at_once = n > cu ? 2 * cu : cu;
     const double per = n > cu ? 3.0 : alone ? 2.5 : 2.0, ends = n <= cu && alone ? 4 : 6.5;
@@ -361,16 +368,17 @@ inline double paged_list_us(int cu, int n_q_heads, int n_kv_heads, int64_t batch
         best = std::min(best, std::ceil(items * parts / cu) * (walk / parts + 12) + 7);
     return 18 + 1.4 * best + (steps ? 9 : 0);
 }
-// Spans: 12 for both launches, and what takes longer, memory or the tiles of a span (2 us each with 64 rows, 1.3 with 32), of which
-// it has enough for the merge's sake (least_span()), and the merge.  (Estimated / measured: 24 x 5 tokens on 10,500, 64 / 8 heads
-// 210 / 187; 41 x 9 on 6,400, 5 / 1 46 / 47; 4 of 540, 32 / 8 14.3 / 11.5.)
+// Spans: 12 for both launches (9.6 with up to 32 rows), and what takes longer, memory or the tiles of a span (2 us each with 64 rows,
+// 1.3 with 32), of which it has enough for the merge's sake (least_span()), and the merge.  (Estimated / measured: 24 x 5 tokens on
+// 10,500, 64 / 8 heads 210 / 187; 41 x 9 on 6,400, 5 / 1 46 / 47; 4 of 540, 32 / 8 11.4 / 11.7; 16 of 2,000 32.6 / 30.7.)
 inline double paged_steps_us(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     const bool few = len_q * group <= 32;
     const double rows = few ? (double)len_q * group : std::min(64.0, (double)len_q * group);
     const double units = n_kv_heads * (len_q * group <= 64 ? (double)batch : (double)total_q * group / 64 + 0.5 * batch);
     const double tiles = units * len_k / 32, merge = len_k / 4096.0 + tiles * rows / 3900;
     const double own = std::max({1.0, tiles / (cu * (few ? 8 : 4)), std::sqrt(merge / 1.3)});
-    return 12 + std::max((double)batch * len_k * n_kv_heads * 512 / 6.0e6, own * (few ? 1.3 : 2.0)) + merge / own;
+    const double memory = (double)batch * len_k * n_kv_heads * 512 / (few ? 6.3e6 : 6.0e6);
+    return (few ? 9.6 : 12) + std::max(memory, own * (few ? 1.3 : 2.0)) + merge / own;
 }
 // Sequences of very different lengths suit a list and spans, which cut them, and not units: these are taken only where even the
 // longest is short, or alone.

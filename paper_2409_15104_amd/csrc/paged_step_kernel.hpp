@@ -20,8 +20,8 @@
 //
 // What bounds it, spans with their merge: memory, 4 sequences of 107,500 tokens, 64 / 8 heads (1.76 GB) 275 us, 6.4 TB/s, as a
 // streaming read; 64 of 27 ... 7,400, 32 / 8 (450 MB) 83 us, of which the merge takes 6; 24 x 5 drafted tokens behind 10,350,
-// 64 / 8, rows of two fragments (1.02 GB) 187 us, 5.7 TB/s while the spans run.  4 of 540, 32 / 8 (9 MB) 11.5 us: launches, three
-// trips to memory each, and three tiles per wavefront.
+// 64 / 8, rows of two fragments (1.02 GB) 187 us, 5.7 TB/s while the spans run.  Units: latency, 4 of 540, 32 / 8 (9 MB), 10.2 us:
+// three trips to memory, then up to three tiles of each wavefront one behind the other, and the join (11.7 as spans with a merge).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
