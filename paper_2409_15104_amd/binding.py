@@ -182,6 +182,19 @@ except ImportError:      # a torch without GPU support, or one that calls these 
         return torch.cuda.current_stream().cuda_stream
 
 
+def _empty(shape, dtype, device, stream, result: bool = True):
+    """Memory for a call on `stream` (None: the current one).  The allocator hands out again at once what the host has freed on the
+    stream that it is asked on, however much of that stream's work with it is still queued: memory for a call on another
+    stream comes from that stream's own, or both work on it at the same time.  A result is held for the current stream too."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _require(t: torch.Tensor, dtype, name: str):
     if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
         raise ValueError("%s must be a contiguous %s tensor on the GPU" % (name, dtype))
@@ -570,14 +583,14 @@ def pec_qk_norm_rope(q, k, norm_rope: NormRope, positions=None, pos0: int = 0, q
     if q is not None:
         q_stride, q_at = _rows(q, "q", index), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+            q_out = _empty(q.shape, _BF16, q.device, stream)
         qo_at = _on(q_out, _BF16, "q_out", index, q.shape)
     if k is not None:
         k_stride, k_at = _rows(k, "k", index), k.data_ptr()
         if k.shape[0] != tokens:
             raise ValueError("q and k must have the same number of tokens")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=_BF16, device=k.device)
+            k_out = _empty(k.shape, _BF16, k.device, stream)
         ko_at = _on(k_out, _BF16, "k_out", index, k.shape)
     at = _on(positions, _I32, "positions", index, (tokens,)) if positions is not None else None
     hkv = given.shape[1] if k is None else k.shape[1]      # (of queries or keys alone: as many of the other)
@@ -603,7 +616,7 @@ def pec_paged_append(k, v, cache: PagedCache, block_table, cu_seqlens_q, seqlens
         if q.shape[0] != tokens:
             raise ValueError("q and k must have the same number of tokens")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+            q_out = _empty(q.shape, _BF16, q.device, stream)
         qo_at = _on(q_out, _BF16, "q_out", index, q.shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -630,17 +643,15 @@ def pec_attn_paged(q, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, m
     q_stride = _rows(q, "q", index)
     total, hq = sizes[0], sizes[1]
     if out is None:
-        out = torch.empty(sizes, dtype=out_dtype, device=q.device)
+        out = _empty(sizes, out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq, total), dtype=_F32, device=q.device)
+        lse = _empty((hq, total), _F32, q.device, stream)
     out_at, lse_at = _on(out, out_dtype, "out", index, sizes), _on(lse, _F32, "lse", index, (hq, total))
     batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, total, max_len_q, max_len_k, index)
     shp = _shape_ref(hq, cache.n_kv_heads, out_dtype, float(scale), int(flags))
     if workspace is None:
         n = int(lib().pec_paged_workspace_bytes(shp, seqlens_k.numel(), total))
-        workspace = torch.empty(max(16, n), dtype=_U8, device=q.device)
-        if stream is not None:      # (not handed out again while that stream still works with it)
-            workspace.record_stream(stream)
+        workspace = _empty(max(16, n), _U8, q.device, stream, result=False)
     _call(lib().pec_attn_paged, "pec_attn_paged", index, stream, shp, cache.ref, batch, q.data_ptr(), q_stride, 1 if causal else 0, out_at,
           lse_at, _on(workspace, _U8, "workspace", index), workspace.numel())
     return out, lse
