@@ -208,9 +208,9 @@ def pec_attn_chunk(q, k, v, q_off: int, kv_off: int, causal: bool = True, out_dt
     sq, hq, d = q.shape
     sk = k.shape[0]
     if out is None:
-        out = torch.empty((sq, hq, d), dtype=out_dtype, device=q.device)
+        out = _empty((sq, hq, d), out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq, sq), dtype=torch.float32, device=q.device)
+        lse = _empty((hq, sq), torch.float32, q.device, stream)
     _require(out, out_dtype, "out")
     _require(lse, torch.float32, "lse")
     shp = _shape(q, k, out_dtype, scale, flags)
@@ -255,7 +255,7 @@ def pec_finalize(o_f32, o_bf16=None, stream=None):
     _require(o_f32, torch.float32, "o_f32")
     sq, hq, d = o_f32.shape
     if o_bf16 is None:
-        o_bf16 = torch.empty((sq, hq, d), dtype=torch.bfloat16, device=o_f32.device)
+        o_bf16 = _empty((sq, hq, d), torch.bfloat16, o_f32.device, stream)
     shp = PecShape(hq, hq, d, PEC_BF16, 0.0, 0)
     _check("pec_finalize", lib().pec_finalize(ctypes.byref(shp), _ptr(o_f32), _ptr(o_bf16), sq, _stream(stream)))
     return o_bf16
@@ -274,14 +274,14 @@ def pec_sp_prefill(q, k, v, q_off: int, chunk: int, causal: bool = True, out_dty
     s_q, hq, d = q.shape
     s_kv = k.shape[0]
     if out is None:
-        out = torch.empty((s_q, hq, d), dtype=out_dtype, device=q.device)
+        out = _empty((s_q, hq, d), out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq, s_q), dtype=torch.float32, device=q.device)
+        lse = _empty((hq, s_q), torch.float32, q.device, stream)
     shp = _shape(q, k, out_dtype, scale, flags)
     if workspace is None:   # only the modes that launch once per ring step keep state between launches
         per_step = flags & (PEC_FLAG_SP_STEP_LAUNCHES | PEC_FLAG_SP_SEPARATE_MERGE)
         nbytes = int(lib().pec_sp_workspace_bytes(ctypes.byref(shp), s_q)) if per_step else 0
-        workspace = torch.empty(max(16, nbytes), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(16, nbytes), torch.uint8, q.device, stream, result=False)
     _check("pec_sp_prefill",
            lib().pec_sp_prefill(ctypes.byref(shp), _ptr(q), _ptr(k), _ptr(v), s_q, int(q_off), s_kv, int(chunk),
                                 int(bool(causal)), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
@@ -354,12 +354,12 @@ def pec_decode_splitkv(q, k, v, n_splits: int = 0, out_dtype=torch.float32, scal
     if n_splits == 0:
         n_splits = int(lib().pec_decode_default_splits(ctypes.byref(shp), sk))
     if out is None:
-        out = torch.empty((1, hq, 128), dtype=out_dtype, device=q.device)
+        out = _empty((1, hq, 128), out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq,), dtype=torch.float32, device=q.device)
+        lse = _empty((hq,), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(max(16, int(lib().pec_decode_workspace_bytes(ctypes.byref(shp), n_splits))),
-                                dtype=torch.uint8, device=q.device)
+        nbytes = int(lib().pec_decode_workspace_bytes(ctypes.byref(shp), n_splits))
+        workspace = _empty(max(16, nbytes), torch.uint8, q.device, stream, result=False)
     _check("pec_decode_splitkv",
            lib().pec_decode_splitkv(ctypes.byref(shp), _ptr(q), _ptr(k), _ptr(v), sk, int(n_splits), _ptr(out),
                                     _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream)))
@@ -387,7 +387,7 @@ def pec_ulysses_layout(x, n_gpus: int, to_messages: bool, out=None, stream=None)
         h = g * hg
         shape = (s, h, d)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+        out = _empty(shape, torch.bfloat16, x.device, stream)
     _check("pec_ulysses_layout", lib().pec_ulysses_layout(_ptr(x), _ptr(out), s, h, d, int(n_gpus),
                                                           int(bool(to_messages)), _stream(stream)))
     return out
@@ -416,13 +416,13 @@ def pec_attn_colocated(q, k, v, cu_seqlens_q, cu_seqlens_k, causal: bool = True,
     total_k = k.shape[0]
     batch = cu_seqlens_q.numel() - 1
     if out is None:
-        out = torch.empty((total_q, hq, d), dtype=out_dtype, device=q.device)
+        out = _empty((total_q, hq, d), out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq, total_q), dtype=torch.float32, device=q.device)
+        lse = _empty((hq, total_q), torch.float32, q.device, stream)
     shp = _shape(q, k, out_dtype, scale, flags)
     if workspace is None:
-        workspace = torch.empty(max(16, int(lib().pec_colocated_workspace_bytes(ctypes.byref(shp), batch, total_q, total_k))),
-                                dtype=torch.uint8, device=q.device)
+        nbytes = int(lib().pec_colocated_workspace_bytes(ctypes.byref(shp), batch, total_q, total_k))
+        workspace = _empty(max(16, nbytes), torch.uint8, q.device, stream, result=False)
     _check("pec_attn_colocated",
            lib().pec_attn_colocated(ctypes.byref(shp), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_q), _ptr(cu_seqlens_k),
                                     batch, total_q, total_k, int(bool(causal)), _ptr(out), _ptr(lse), _ptr(workspace),
@@ -460,11 +460,11 @@ def pec_attn_varlen(q, k, v, cu_seqlens, max_seqlen: int, causal: bool = True, o
     total, hq, d = q.shape
     batch = cu_seqlens.numel() - 1
     if out is None:
-        out = torch.empty((total, hq, d), dtype=out_dtype, device=q.device)
+        out = _empty((total, hq, d), out_dtype, q.device, stream)
     if lse is None:
-        lse = torch.empty((hq, total), dtype=torch.float32, device=q.device)
+        lse = _empty((hq, total), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(max(16, pec_varlen_workspace_bytes(batch, total)), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(16, pec_varlen_workspace_bytes(batch, total)), torch.uint8, q.device, stream, result=False)
     shp = _shape(q, k, out_dtype, scale, flags)
     _check("pec_attn_varlen",
            lib().pec_attn_varlen(ctypes.byref(shp), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), batch, total,

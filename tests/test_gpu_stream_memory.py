@@ -58,3 +58,20 @@ def test_norm_rope_and_append():
         return (qa, *pec.pec_qk_norm_rope(q, kv, turn, stream=s))
 
     two_at_once(call, inputs(3), inputs(4))
+
+
+def test_batches_of_keys_in_a_row():
+    """pec_attn_colocated, pec_attn_varlen and pec_decode_splitkv, each with a workspace, and pec_attn_chunk."""
+    lens_q, lens_k = [1, 300, 1], [9000, 2000, 4000]
+    cu = [torch.tensor([0] + x, dtype=torch.int64).cumsum(0).to(torch.int32).to(DEV) for x in (lens_q, lens_k)]
+
+    def inputs(seed):
+        g = torch.Generator().manual_seed(seed)
+        return [torch.randn(n, h, 128, generator=g).to(torch.bfloat16).to(DEV) for n, h in ((sum(lens_q), 8), (sum(lens_k), 2), (sum(lens_k), 2))]
+
+    def call(x, s):
+        q, k, v = x
+        return (*pec.pec_attn_colocated(q, k, v, *cu, stream=s), *pec.pec_attn_varlen(q, k[:302].contiguous(), v[:302].contiguous(), cu[0], 300, stream=s),
+                *pec.pec_decode_splitkv(q[:1].contiguous(), k, v, stream=s), *pec.pec_attn_chunk(q, k, v, 14000, 0, stream=s))
+
+    two_at_once(call, inputs(5), inputs(6))

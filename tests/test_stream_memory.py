@@ -61,14 +61,25 @@ PAGED = {
     "pec_paged_append": lambda **kw: pec.pec_paged_append(rows(5, 2), rows(5, 2), CACHE, *META, q=rows(5, 4), **kw),
     "pec_attn_paged": lambda **kw: pec.pec_attn_paged(rows(5, 4), CACHE, *META, **kw),
 }
+CU = torch.zeros(4, dtype=I32)
+IN_A_ROW = {
+    "pec_attn_chunk": lambda **kw: pec.pec_attn_chunk(rows(5, 4), rows(9, 2), rows(9, 2), 4, 0, **kw),
+    "pec_finalize": lambda **kw: pec.pec_finalize(rows(5, 4), **kw),
+    "pec_sp_prefill": lambda **kw: pec.pec_sp_prefill(rows(5, 4), rows(9, 2), rows(9, 2), 0, 5, flags=pec.PEC_FLAG_SP_STEP_LAUNCHES, **kw),
+    "pec_decode_splitkv": lambda **kw: pec.pec_decode_splitkv(rows(1, 4), rows(9, 2), rows(9, 2), **kw),
+    "pec_ulysses_layout": lambda **kw: pec.pec_ulysses_layout(rows(4, 4), 2, True, **kw),
+    "pec_attn_colocated": lambda **kw: pec.pec_attn_colocated(rows(5, 4), rows(9, 2), rows(9, 2), CU, CU, **kw),
+    "pec_attn_varlen": lambda **kw: pec.pec_attn_varlen(rows(5, 4), rows(5, 2), rows(5, 2), CU, 5, **kw),
+}
+CALLS = {**PAGED, **IN_A_ROW}
 
 
-@pytest.mark.parametrize("name", PAGED)
+@pytest.mark.parametrize("name", CALLS)
 def test_memory_of_a_call_is_its_streams(world, name):
-    PAGED[name](stream=S)
+    CALLS[name](stream=S)
     assert world.allocated and all(stream is S for _, stream in world.allocated)
-    # results are held for the stream that they are read on, a workspace for no other
-    assert world.held == [(shape, "current") for shape, _ in world.allocated if len(shape) > 1]
+    # results are held for the stream that they are read on, a workspace (16 bytes: its size is 0 here) for no other
+    assert world.held == [(shape, "current") for shape, _ in world.allocated if shape != (16,)]
     n = len(world.allocated)
-    PAGED[name]()
+    CALLS[name]()
     assert len(world.allocated) == 2 * n and all(stream is None for _, stream in world.allocated[n:])
