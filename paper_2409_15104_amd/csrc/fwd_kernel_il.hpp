@@ -65,6 +65,8 @@ __device__ __forceinline__ void scale_acc_in_place(f32x16 (&o)[4], float a) {
 // kFwdPaged -- a work list over keys and values in pages: an item is a sequence's query tile and a range of its keys.
 enum { kFwdDense = 0, kFwdSweep = 1, kFwdList = 2, kFwdSpan = 3, kFwdPaged = 4 };
 
+__device__ const u32x4 kZeroRow[16] = {};      // what the values past the end of a paged sequence are read from
+
 template <int MODE>
 __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     constexpr bool kSweep = MODE == kFwdSweep;
@@ -522,7 +524,10 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
                 const uint32_t col = is_v ? (uint32_t)((((r_pos >> 2) ^ (key & 3)) << 2) | (r_pos & 3)) * 16u
                                           : (uint32_t)(r_pos ^ (key & 15)) * 16u;
                 const int from = min(tile * kBN + 4 * (it * NWAVES + wave), last & ~3);      // four keys of one page
-                dma16<false>(base_of(it, from), (uint32_t)(min(tile * kBN + key, last) - from) * kv_stride_b + col, lds0 + it * NWAVES * 1024);
+                if (!is_v || tile * kBN + key <= last)
+                    dma16<false>(base_of(it, from), (uint32_t)(min(tile * kBN + key, last) - from) * kv_stride_b + col, lds0 + it * NWAVES * 1024);
+                else   // zero: the last value over again, were it infinite, would make NaN of its weight of 0 (512 new tokens 0.6 % longer)
+                    dma16<false>(reinterpret_cast<const unsigned char*>(kZeroRow), (uint32_t)r_pos * 16u, lds0 + it * NWAVES * 1024);
             }
         }
     };
