@@ -37,6 +37,7 @@ struct NormRopeParams {
 };
 
 constexpr int kNormRopeThreads = 256;
+constexpr int kNormRopeRow = 1 << 23;        // workgroups in a row of the grid: a dimension of a launch counts its threads in 32 bits
 __device__ __forceinline__ float row_rotated(float x, int ctrl) {     // 16 lanes rotated among themselves; ctrl is a constant
     switch (ctrl) {
         case 1: return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x121, 0xf, 0xf, true));
@@ -53,7 +54,8 @@ enum { kPairsNone = 0, kPairsFar = 1, kPairsHalf = 2, kPairsNext = 3 };
 template <bool NORM, int PAIRS, bool APPEND>
 __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormRopeParams p) {
     const int lane = threadIdx.x & 63, c = lane & 15, sub = lane >> 4;
-    const int64_t w = (int64_t)blockIdx.x * (kNormRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t w = ((int64_t)blockIdx.y * kNormRopeRow + blockIdx.x) * (kNormRopeThreads / 64) +
+                      __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int token = (int)(w / p.parts), part = (int)(w % p.parts);
     if (token >= p.tokens) return;
     // groups of four head rows: queries, keys, values

@@ -112,8 +112,7 @@ int launch_norm_rope(NormRopeParams& p, bool append, hipStream_t st) {
     p.parts = norm_rope_parts(compute_units(), p.tokens, (p.n_q_heads + 3) / 4 + (append ? 2 : 1) * ((p.n_kv_heads + 3) / 4));
     const int64_t waves = (int64_t)p.tokens * p.parts;
     const int64_t blocks = (waves + kNormRopeThreads / 64 - 1) / (kNormRopeThreads / 64);
-    if (blocks > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, kNormRopeRow), (unsigned)((blocks + kNormRopeRow - 1) / kNormRopeRow));
     const bool norm = p.q_weight || p.k_weight;
     if (append && norm) launch_norm_rope<true, true>(p, grid, st);
     else if (append) launch_norm_rope<false, true>(p, grid, st);
