@@ -232,7 +232,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         s.cut = StepCut{fast_div(g), 5, p.causal, 0x7fffffff};
         const int64_t groups = (batch->total_q * g / 32 + batch->batch) * p.n_kv_heads;
         if (groups > 0x7fffff00) return PEC_ERR_UNSUPPORTED;
-        const dim3 grid((unsigned)((groups + 7) / 8 * 8));
+        const dim3 grid((unsigned)std::min<int64_t>((groups + 7) / 8 * 8, kUnitsRow), (unsigned)((groups + kUnitsRow - 1) / kUnitsRow));
         if (cut.unit_waves == 4)
             hipLaunchKernelGGL((paged_step_kernel<1, 4, 1, true>), grid, dim3(4 * 64), 0, st, s);
         else

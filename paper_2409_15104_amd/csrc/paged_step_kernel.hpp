@@ -34,6 +34,7 @@ namespace pec {
 constexpr int kPagedWaves1 = 8, kPagedWaves2 = 4;     // wavefronts per workgroup of up to 32 and up to 64 rows a unit
 constexpr int kStepTile = 32;
 constexpr int kStepTileBytes = kStepTile * kRowBytes;
+constexpr int kUnitsRow = 1 << 22;                     // workgroups in a row of the units' grid, whose dimensions count threads in 32 bits
 constexpr int kPagedChunks = 1024;                     // sequences are added up 64 at a time: up to 65,536 of them
 
 // Sums that stop at kTooMany: the host refuses calls of so many steps, but offsets that fall can make sequences overlap, and
@@ -227,8 +228,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     int at, left, kvh, w = 0;               // place on the line, tiles to work on
     if constexpr (SHARED) {
         const WorkOrder order(line.total, 1, p.a.n_kv_heads);
-        if ((blockIdx.x >> 3) >= order.count || order.total > gridDim.x) return;      // (more units than the rows make: as above)
-        const int64_t unit = order.unit(blockIdx.x & 7, blockIdx.x >> 3);
+        const uint32_t block = blockIdx.y * kUnitsRow + blockIdx.x;
+        if ((block >> 3) >= order.count || order.total > (int64_t)gridDim.x * gridDim.y) return;      // (more units than the rows make: as above)
+        const int64_t unit = order.unit(block & 7, block >> 3);
         if (unit < 0) return;
         kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
         at = __builtin_amdgcn_readfirstlane((int)unit - kvh * line.total);

@@ -44,3 +44,28 @@ def test_append():
     where = table.long()[at // 256].to(DEV), (at % 256).to(DEV)
     want = x[at.to(DEV)].view(torch.int16)
     assert bool((kc[where].view(torch.int16) == want).all()) and bool((vc[where].view(torch.int16) == want).all())
+
+
+# (the hints choose units: tests/test_many_tokens_path.py)
+SEQUENCES, HEADS, HINTS, TABLE = 16384, 1024, (300, 3000), 400
+
+
+def test_attention_of_many_heads():
+    """A workgroup for every sequence and KV head, 17 million of them: a sequence of one token gets its value and its score."""
+    g = torch.Generator(DEV).manual_seed(6)
+    pages = 64
+    kc, vc = [torch.empty(pages, 8, HEADS, 128, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2)]
+    q = torch.empty(SEQUENCES, HEADS, 128, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    table = torch.full((SEQUENCES, TABLE), -1, dtype=torch.int32, device=DEV)
+    table[:, 0] = torch.randint(0, pages, (SEQUENCES,), generator=g, device=DEV, dtype=torch.int32)
+    cu = torch.arange(SEQUENCES + 1, dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((HEADS, SEQUENCES), 7.0, device=DEV)
+    pec.pec_attn_paged(q, pec.PagedCache(kc, vc), table, cu, torch.ones(SEQUENCES, dtype=torch.int32, device=DEV), *HINTS, out=out, lse=lse)
+    for r in range(0, SEQUENCES, 2048):
+        number = table[r:r + 2048, 0].long()
+        assert bool((out[r:r + 2048].view(torch.int16) == vc[number, 0].view(torch.int16)).all())
+        product = q[r:r + 2048].double() * kc[number, 0].double() * 128 ** -0.5
+        want = product.sum(dim=-1).T
+        allowed = 2 * (128 * ref.F32 * product.abs().sum(dim=-1).T + 2.0 ** -20) + 2.0 ** -20 * want.abs()
+        assert bool(((lse[:, r:r + 2048].double() - want).abs() <= allowed).all())
