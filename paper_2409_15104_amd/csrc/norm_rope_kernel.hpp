@@ -138,6 +138,8 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
     }
 
     // ---- head rows, four at a time; the weights of their kind go into the angles
+    constexpr float kSmallMean = 0x1p-100f;
+    const bool small_eps = __builtin_bit_cast(uint32_t, p.eps) < __builtin_bit_cast(uint32_t, kSmallMean);      // (it is not negative)
     float a[8], b[8];
     bool normed = false;
     int kind_now = -1;
@@ -176,14 +178,24 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                 }
                 float inv = 1.f;
                 if (NORM && normed) {
-                    float ss = 0.f;
+                    auto mean = [&](float eps) {      // of the squares, and eps
+                        float ss = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-                    ss += row_rotated(ss, 8);
-                    ss += row_rotated(ss, 4);
-                    ss += row_rotated(ss, 2);
-                    ss += row_rotated(ss, 1);
-                    inv = __builtin_amdgcn_rsqf(fmaf(ss, 1.f / kHeadDim, p.eps));
+                        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+                        ss += row_rotated(ss, 8);
+                        ss += row_rotated(ss, 4);
+                        ss += row_rotated(ss, 2);
+                        ss += row_rotated(ss, 1);
+                        return fmaf(ss, 1.f / kHeadDim, eps);
+                    };
+                    float m = mean(p.eps);
+                    if (small_eps) {      // rows whose squares may be too small for fp32, and their mean for v_rsq_f32, a factor larger
+                        const float up = m < kSmallMean ? 1.f / kSmallMean : 1.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] *= up;
+                        m = mean(p.eps * up * up);
+                    }
+                    inv = __builtin_amdgcn_rsqf(m);
                 }
                 float z[8];
 #pragma unroll
