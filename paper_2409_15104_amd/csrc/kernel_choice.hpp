@@ -327,7 +327,9 @@ inline int64_t decode_default_ranges(int cu, int n_q_heads, int n_kv_heads, int6
 // Which kernels a paged call runs on.  `units`: a workgroup of paged_step_kernel for every 32 rows of a KV head, nothing else;
 // `steps`: its spans and their merge, for sequences with few rows per KV head (32 nt); `list`: the pipelined kernel's work list for
 // the others, or for all.  The host knows no lengths but the caller's hints (len_q, len_k: the longest), so these are estimates
-// for sequences that are all as long, in microseconds, fitted to 40 random calls on 256 compute units.
+// for sequences that are all as long, in microseconds, on 256 compute units: units of several to a sequence and the list after 130
+// random calls, single units and spans after 477 more.  64 others, each timed in every way that suits it: the chosen one took 2.2 %
+// longer than the fastest on the mean, 29 % at most (2 x 80 new tokens behind 10,500, 24 / 8 heads: 87 as spans, 67 as a list).
 constexpr int kPagedFewRows = 64;
 struct PagedCut {
     bool units, steps, list;
@@ -339,8 +341,8 @@ struct PagedCut {
 // few row tiles) and, per 256 keys, 2 (2.5 where nobody else reads them) or 3.  (Estimated / measured: 953 new tokens, 5 / 1 heads
 // 17.5 / 14.7; 5,189, 1 / 1 51 / 48; 1,472 behind 1,400, 12 / 4 54 / 58; 1,245, 20 / 4 25 / 26.)
 // One unit per sequence and KV head, which has its keys to itself: 2.05 per 256 keys, or 7.5 a round, against memory.  (477 calls of
-// 1 ... 128 sequences on 60 ... 3,300 keys, with units and with spans: the mean estimate is off by 7 %, the choice costs 0.3 % on the
-// mean.  4 of 540, 32 / 8 heads, 10.2 as units, 11.7 as spans; of 1,000 14.9 and 12.8; 32 of 1,000 23.5 and 31.0.)
+// 1 ... 128 sequences on 60 ... 3,300 keys, with units and with spans: the mean estimate is off by 7 %, the choice between the two
+// costs 0.3 % on the mean.  4 of 540, 32 / 8 heads, 10.2 as units, 11.7 as spans; of 1,000 14.9 and 12.8; 32 of 1,000 23.5 and 31.0.)
 inline double paged_units(int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q) {
     return n_kv_heads * (len_q * group <= 32 ? (double)batch : (double)total_q * group / 32 + 0.5 * batch);
 }
@@ -401,7 +403,8 @@ inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, 
     return c;
 }
 
-// Wavefronts per token of norm_rope_kernel, each with an equal part of the token's groups of four head rows.
+// Wavefronts per token of norm_rope_kernel, each with as many of the token's groups of four head rows as the first (rounded up, so that
+// the last may have fewer or none: 4 groups for 3 wavefronts are 2, 2 and none).
 inline int norm_rope_parts(int cu, int64_t tokens, int64_t quads) {
     const int64_t wanted = ((int64_t)cu * 16 + tokens - 1) / std::max<int64_t>(1, tokens);
     return (int)std::max<int64_t>(1, std::min(quads, wanted));
