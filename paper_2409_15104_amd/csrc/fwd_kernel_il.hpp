@@ -526,7 +526,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
                 const int from = min(tile * kBN + 4 * (it * NWAVES + wave), last & ~3);      // four keys of one page
                 if (!is_v || tile * kBN + key <= last)
                     dma16<false>(base_of(it, from), (uint32_t)(min(tile * kBN + key, last) - from) * kv_stride_b + col, lds0 + it * NWAVES * 1024);
-                else   // zero: the last value over again, were it infinite, would make NaN of its weight of 0 (512 new tokens 0.6 % longer)
+                else   // zero: the last value over again, were it infinite, would make NaN of its weight of 0
                     dma16<false>(reinterpret_cast<const unsigned char*>(kZeroRow), (uint32_t)r_pos * 16u, lds0 + it * NWAVES * 1024);
             }
         }
@@ -1066,7 +1066,7 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
     if constexpr (kPaged) {
         if (odd_rows != 0) {
             // Only if a key that the wavefront's first row does not see has such a value (else they are what they are): the
-            // rows are worked out again, plainly.  As slow as it is rare: at most the rows of the tiles that hold such a key.
+            // wavefront's rows are worked out again, by themselves.
             const PagedKv cache{reinterpret_cast<unsigned char*>(const_cast<__bf16*>(p.k)), reinterpret_cast<unsigned char*>(const_cast<__bf16*>(p.v)),
                                 p.page_b, p.row_b, p.head_b, p.last_page, p.log_page};
             const int32_t* const table_row = p.table + (int64_t)g.seq * p.table_len;
@@ -1080,16 +1080,25 @@ __global__ __launch_bounds__(512) void fwd_il_kernel(const FwdParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) found |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
             }
-            if (!__any(found)) odd_rows = 0;
-            __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt 0: the rows' first results are in place
-            for (; odd_rows != 0; odd_rows &= odd_rows - 1) {
-                const int row = rw0 + __builtin_ctzll(odd_rows);
-                const __bf16* const qv = p.q + g.q_off0 + row * g.q_stride + 2 * lane;
-                const PlainRow fixed = plain_row(cache, table_row, g.kvh, (float)qv[0], (float)qv[1], p.scale_log2 * kLn2, first,
-                                                 first + max(0, min(sk, row + delta + 1)));
-                const int64_t idx = o_off0 + row * q_stride + 2 * lane;
-                if (out_f32) *reinterpret_cast<f32x2*>(reinterpret_cast<float*>(out_ptr) + idx) = f32x2{fixed.o0, fixed.o1};
-                else *reinterpret_cast<bf16x2*>(reinterpret_cast<__bf16*>(out_ptr) + idx) = __builtin_convertvector(f32x2{fixed.o0, fixed.o1}, bf16x2);
+            if (__any(found)) {
+                __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt 0: the rows' first results are in place
+                const int ln = lane_id(), row = rw0 + (ln & 31);
+                f32x16 again[4];
+                rows_again(cache, table_row, g.kvh, p.q + g.q_off0 + row * g.q_stride, row < sq, p.scale_log2, first,
+                           min(sk, max(0, wave_last + delta + 1)), rw0 + delta, row + delta, again);
+                if (odd_rows >> (ln & 31) & 1) {
+                    const int64_t idx = o_off0 + row * q_stride + 4 * (ln >> 5);
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            f32x4 x;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] = again[dt][4 * b + i];
+                            if (out_f32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out_ptr) + idx + 32 * dt + 8 * b) = x;
+                            else *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(out_ptr) + idx + 32 * dt + 8 * b) = __builtin_convertvector(x, bf16x4);
+                        }
+                }
             }
         }
     }
