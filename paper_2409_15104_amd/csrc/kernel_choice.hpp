@@ -328,8 +328,8 @@ inline int64_t decode_default_ranges(int cu, int n_q_heads, int n_kv_heads, int6
 // `steps`: its spans and their merge, for sequences with few rows per KV head (32 nt); `list`: the pipelined kernel's work list for
 // the others, or for all.  The host knows no lengths but the caller's hints (len_q, len_k: the longest), so these are estimates
 // for sequences that are all as long, in microseconds, on 256 compute units: units of several to a sequence and the list after 130
-// random calls, single units and spans after 477 more.  64 others, each timed in every way that suits it: the chosen one took 2.2 %
-// longer than the fastest on the mean, 29 % at most (2 x 80 new tokens behind 10,500, 24 / 8 heads: 87 as spans, 67 as a list).
+// random calls, single units and spans after 477 more.  64 others, each timed in every way that suits it: the chosen one took 2.8 %
+// longer than the fastest on the mean, 35 % at most (2 x 80 new tokens behind 10,500, 24 / 8 heads: 87 as spans, 65 as a list).
 constexpr int kPagedFewRows = 64;
 struct PagedCut {
     bool units, steps, list;
