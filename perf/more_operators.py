@@ -1,0 +1,372 @@
+"""Operators of a paged cache that holds keys and values in 4 bits: a value is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, times
+a power of two that 32 dims of a head row share.  New tokens on their way into such a cache (`append`: rounded, stored and read back,
+as a prompt does that goes on with the values which later steps will see), stored tokens read back into packed rows (`read`), and
+attention of every sequence's new tokens over its pages (`attn`).
+
+`listed()` are the cases that are timed, `draw()` makes more of the same ranges, `prepare()` makes what a server holds ahead of
+the call, `run()` makes the call (the framework's with `own`, elementary torch operations in 32 bits without), `work()` counts
+what it cannot do without, `exact()` is the definition in 64 bits.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda"
+DIM, GROUP = 128, 32        # head dim of the framework; dims that share a scale
+ROW_BYTES = DIM / 2 + DIM / GROUP
+LARGEST_FLOPS = 8.5e12      # no drawn case costs more than the largest listed ones
+LARGEST_BYTES = 6.5e8
+
+
+# ---- cases
+
+def _case(op, name, hq, hkv, page, lengths, steps=0, step_q=1, ctx=0, spread=False, chunks=0, chunk_q=0, chunk_ctx=0, by_head=False,
+          causal=True):
+    """`steps` sequences with `step_q` new tokens on about `ctx` cached ones (spread: log-normal around it, up to 12 times as
+    many), then `chunks` sequences with about `chunk_q` new tokens behind about `chunk_ctx` cached ones.  `lengths` seeds them.
+    `read` reads the new tokens back."""
+    return {"op": op, "name": name, "hq": hq, "hkv": hkv, "page": page, "lengths": lengths, "steps": steps, "step_q": step_q,
+            "ctx": ctx, "spread": spread, "chunks": chunks, "chunk_q": chunk_q, "chunk_ctx": chunk_ctx, "by_head": by_head,
+            "causal": causal}
+
+
+def listed():
+    return [
+        # one decode step of a nearly idle server: all latency
+        _case("attn", "attn_step_few", 32, 8, 16, 31, steps=4, ctx=600),
+        # one decode step of a busy one, contexts as the short prompts of the paper's trace
+        _case("attn", "attn_step_batch", 32, 8, 16, 32, steps=64, ctx=700, spread=True),
+        # decode steps of long requests, many heads, large pages: what a cache in 4 bits is for
+        _case("attn", "attn_step_long", 64, 8, 256, 33, steps=4, ctx=131072),
+        # more requests at once than a cache of 16 bits has room for, laid out by heads
+        _case("attn", "attn_step_many", 32, 8, 32, 34, steps=120, ctx=3900, by_head=True),
+        # five drafted tokens of every sequence looked at together
+        _case("attn", "attn_verify", 64, 8, 32, 35, steps=24, step_q=5, ctx=12000),
+        # one chunk of a long prompt, small enough not to hold up the decode steps beside it
+        _case("attn", "attn_chunk_512", 32, 8, 64, 36, chunks=1, chunk_q=512, chunk_ctx=30000),
+        # a chunk as large as the segments of the sequence-parallel prefill
+        _case("attn", "attn_chunk_8k", 32, 8, 64, 37, chunks=1, chunk_q=8192, chunk_ctx=57000),
+        # short prompts without a prefix beside decode steps
+        _case("attn", "attn_mixed", 32, 8, 16, 38, steps=24, ctx=3500, spread=True, chunks=6, chunk_q=1100, chunk_ctx=0, by_head=True),
+        # a step's new keys and values
+        _case("append", "append_step", 32, 8, 16, 41, steps=64, ctx=450),
+        # chunks of three prompts
+        _case("append", "append_chunks", 32, 8, 64, 42, chunks=3, chunk_q=2700, chunk_ctx=5000, by_head=True),
+        # the prefix that a few new prompts share, for attention on keys in a row
+        _case("read", "read_prefix", 32, 8, 16, 43, chunks=1, chunk_q=1931, chunk_ctx=0),
+        # long requests that move to another GPU
+        _case("read", "read_long", 64, 8, 64, 44, chunks=4, chunk_q=30000, chunk_ctx=0, by_head=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    while True:
+        hkv = rng.choice([1, 2, 4, 8])
+        hq = hkv * rng.choice([1, 2, 3, 4, 5, 8])
+        page = rng.choice([16, 32, 64, 128, 256])
+        lengths = rng.randrange(1 << 20)
+        by_head = rng.random() < 0.3
+        kind = rng.choice(["step", "step", "step", "verify", "chunk", "chunk", "mixed", "append", "append", "read", "read"])
+        if kind == "step":
+            c = _case("attn", "", hq, hkv, page, lengths, steps=_log(rng, 1, 128), ctx=_log(rng, 64, 131072), spread=rng.random() < 0.5,
+                      by_head=by_head)
+        elif kind == "verify":
+            c = _case("attn", "", hq, hkv, page, lengths, steps=_log(rng, 1, 48), step_q=rng.randint(2, 9), ctx=_log(rng, 64, 16384),
+                      by_head=by_head)
+        elif kind == "chunk":
+            c = _case("attn", "", hq, hkv, page, lengths, chunks=rng.randint(1, 4), chunk_q=_log(rng, 64, 8192),
+                      chunk_ctx=_log(rng, 1, 57000), by_head=by_head, causal=rng.random() < 0.85)
+        elif kind == "mixed":
+            c = _case("attn", "", hq, hkv, page, lengths, steps=_log(rng, 1, 48), ctx=_log(rng, 64, 16384), spread=True,
+                      chunks=rng.randint(1, 6), chunk_q=_log(rng, 32, 2048), chunk_ctx=rng.choice([0, _log(rng, 1, 8192)]),
+                      by_head=by_head)
+        elif kind == "append" and rng.random() < 0.5:
+            c = _case("append", "", hq, hkv, page, lengths, steps=_log(rng, 1, 128), step_q=rng.choice([1, 1, 4]), ctx=_log(rng, 16, 500),
+                      by_head=by_head)
+        else:
+            c = _case(kind, "", hq, hkv, page, lengths, chunks=rng.randint(1, 4), chunk_q=_log(rng, 16, 4096 if kind == "append" else 30000),
+                      chunk_ctx=_log(rng, 1, 4096), by_head=by_head)
+        w = work(c)
+        if w["flops"] <= LARGEST_FLOPS and w["bytes"] <= LARGEST_BYTES:
+            del c["name"]
+            return c
+
+
+def _lengths(case):
+    """New tokens and cached tokens (the new ones among them) of every sequence."""
+    rng = random.Random(case["lengths"])
+    new, total = [], []
+    for _ in range(case["steps"]):
+        if case["spread"]:
+            n = int(round(case["ctx"] * math.exp(1.27 * rng.gauss(0.0, 1.0))))
+            n = max(1, min(n, 12 * case["ctx"]))
+        else:
+            n = rng.randint(max(1, int(0.7 * case["ctx"])), case["ctx"])
+        new.append(case["step_q"])
+        total.append(n + case["step_q"])
+    for _ in range(case["chunks"]):
+        n = case["chunk_q"] if case["chunks"] == 1 else rng.randint(max(1, case["chunk_q"] // 2), case["chunk_q"])
+        ctx = rng.randint(int(0.9 * case["chunk_ctx"]), case["chunk_ctx"]) if case["chunk_ctx"] else 0
+        new.append(n)
+        total.append(n + ctx)
+    order = list(range(len(new)))
+    rng.shuffle(order)
+    return [new[i] for i in order], [total[i] for i in order]
+
+
+# ---- the format, in elementary operations
+
+LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _codes(x):
+    """fp32 [..., 128] -> 4-bit codes [..., 128] (the sign in bit 3) and scale bytes [..., 4]: the power of two by which the group's
+    largest magnitude, rounded to two significant bits, is 4 or 6 (2^-125 ... 2^125, byte = exponent + 127)."""
+    g = x.unflatten(-1, (-1, GROUP))
+    m, e = torch.frexp(g.abs().amax(dim=-1))                       # m in [0.5, 1)
+    e = (e - 3 + (m >= 0.875).int()).clamp(-125, 125)
+    e = torch.where(m == 0, -125, e)
+    y = torch.ldexp(g, -e[..., None]).abs()                        # exact
+    code = torch.zeros(y.shape, dtype=torch.uint8, device=x.device)
+    for border, tie_up in ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False), (3.5, True), (5.0, False)):
+        code += y >= border if tie_up else y > border
+    code += 8 * torch.signbit(g).to(torch.uint8)
+    return code.flatten(-2), (e + 127).to(torch.uint8)
+
+
+def _packed(code):
+    return code[..., 0::2] | code[..., 1::2] << 4
+
+
+def _values(packed, scale):
+    """Codes [..., 64] and scale bytes [..., 4] -> fp32 [..., 128]."""
+    levels = torch.tensor(LEVELS + tuple(-x for x in LEVELS), dtype=torch.float32, device=packed.device)
+    code = torch.stack([packed & 15, packed >> 4], dim=-1).flatten(-2)
+    factor = torch.exp2(scale.float() - 127.0)
+    return (levels[code.int()].unflatten(-1, (-1, GROUP)) * factor[..., None]).flatten(-2)
+
+
+# ---- inputs
+
+def _randn(gen, *shape):
+    return torch.randn(*shape, generator=gen, device=DEV, dtype=torch.float32).to(torch.bfloat16)
+
+
+def _pool(gen, n_pages, page, hkv, by_head):
+    """Codes [n_pages, page, hkv, 64] and scales [n_pages, hkv, 4, page] of normal values; the last eighth of the heads' dims is larger, as
+    the keys of models are."""
+    codes = torch.empty((n_pages, hkv, page, DIM // 2) if by_head else (n_pages, page, hkv, DIM // 2), dtype=torch.uint8, device=DEV)
+    codes = codes.transpose(1, 2) if by_head else codes
+    scales = torch.empty(n_pages, hkv, DIM // GROUP, page, dtype=torch.uint8, device=DEV)
+    size = torch.ones(DIM, device=DEV)
+    size[DIM - DIM // 8:] = 2.0
+    step = max(1, (1 << 27) // (page * hkv * DIM))
+    for p in range(0, n_pages, step):
+        n = min(step, n_pages - p)
+        c, s = _codes(_randn(gen, n, page, hkv, DIM).float() * size)
+        codes[p:p + n] = _packed(c)
+        scales[p:p + n] = s.permute(0, 2, 3, 1)
+    return codes, scales
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    host = random.Random(seed)
+    hq, hkv, page = case["hq"], case["hkv"], case["page"]
+    st = {"case": dict(case)}
+    new, total = _lengths(case)
+    n = sum(new)
+    need = [-(-t // page) for t in total]
+    n_pages = sum(need) + max(2, sum(need) // 16)
+    st["k_cache"], st["k_scale"] = _pool(gen, n_pages, page, hkv, case["by_head"])
+    st["v_cache"], st["v_scale"] = _pool(gen, n_pages, page, hkv, case["by_head"])
+    numbers = list(range(n_pages))
+    host.shuffle(numbers)
+    rows, at = [], 0
+    for m in need:      # behind a sequence's last page the table holds whatever was there
+        rows.append(numbers[at:at + m] + [host.randrange(n_pages) for _ in range(max(need) - m)])
+        at += m
+    st["block_table"] = torch.tensor(rows, dtype=torch.int32, device=DEV)
+    starts = [0]
+    for m in new:
+        starts.append(starts[-1] + m)
+    st["cu_q"] = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    st["len_k"] = torch.tensor(total, dtype=torch.int32, device=DEV)
+    st["new"], st["total"] = new, total
+    if case["op"] == "attn":
+        st["q"] = _randn(gen, n, hq, DIM)
+        st["out"] = torch.empty(n, hq, DIM, dtype=torch.bfloat16, device=DEV)
+        st["lse"] = torch.empty(hq, n, dtype=torch.float32, device=DEV)
+    else:
+        if case["op"] == "append":      # parts of one projection's output
+            qkv = _randn(gen, n, hq + 2 * hkv, DIM)
+            st["k"], st["v"] = qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+        st["k_out"] = torch.empty(n, hkv, DIM, dtype=torch.bfloat16, device=DEV)
+        st["v_out"] = torch.empty(n, hkv, DIM, dtype=torch.bfloat16, device=DEV)
+    return st
+
+
+# ---- one pass
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"attn": _plain_attn, "append": _plain_append, "read": _plain_read}[state["case"]["op"]](state)
+
+
+def _run_own(st):
+    from paper_2409_15104_amd import binding as pec
+
+    case = st["case"]
+    if "handles" not in st:     # made once by a server: the cache, a workspace with room for the chunks' keys
+        cache = pec.PagedCacheFp4(st["k_cache"], st["v_cache"], st["k_scale"], st["v_scale"])
+        workspace = None
+        if case["op"] == "attn":
+            chunk_keys = sum(t for m, t in zip(st["new"], st["total"]) if m > case["step_q"]) if case["chunks"] else 0
+            size = pec.pec_paged_fp4_workspace_bytes(case["hq"], case["hkv"], len(st["new"]), sum(st["new"]), chunk_keys)
+            workspace = torch.empty(size, dtype=torch.uint8, device=DEV)
+        st["handles"] = cache, workspace
+    cache, workspace = st["handles"]
+    if case["op"] == "attn":
+        pec.pec_attn_paged_fp4(st["q"], cache, st["block_table"], st["cu_q"], st["len_k"], max_len_q=max(st["new"]),
+                               max_len_k=max(st["total"]), causal=case["causal"], out_dtype=st["out"].dtype, out=st["out"],
+                               lse=st["lse"], workspace=workspace)
+        return st["out"], st["lse"]
+    if case["op"] == "append":
+        pec.pec_paged_append_fp4(st["k"], st["v"], cache, st["block_table"], st["cu_q"], st["len_k"])
+    return pec.pec_paged_read_fp4(cache, st["block_table"], st["cu_q"], st["len_k"], k=st["k_out"], v=st["v_out"])
+
+
+def _places(st):
+    """Page and slot of every packed row."""
+    page = st["case"]["page"]
+    cu, len_k = st["cu_q"].long(), st["len_k"].long()
+    token = torch.arange(st["k_out"].shape[0], device=DEV)
+    seq = torch.bucketize(token, cu[1:], right=True)
+    at = len_k[seq] - cu[seq + 1] + token
+    return st["block_table"].long()[seq, at // page], at % page
+
+
+def _plain_append(st):
+    number, slot = _places(st)
+    for x, codes, scales in ((st["k"], st["k_cache"], st["k_scale"]), (st["v"], st["v_cache"], st["v_scale"])):
+        c, s = _codes(x.float())
+        codes[number, slot] = _packed(c)
+        scales[number, :, :, slot] = s
+    return _plain_read(st)
+
+
+def _plain_read(st):
+    number, slot = _places(st)
+    return tuple(_values(codes[number, slot], scales[number, :, :, slot]).to(torch.bfloat16)
+                 for codes, scales in ((st["k_cache"], st["k_scale"]), (st["v_cache"], st["v_scale"])))
+
+
+def _plain_attn(st):
+    case = st["case"]
+    hq, hkv, page = case["hq"], case["hkv"], case["page"]
+    g, scale = hq // hkv, 1.0 / math.sqrt(DIM)
+    out = torch.empty_like(st["out"])
+    lse = torch.empty_like(st["lse"])
+    q0 = 0
+    for b, (nq, nk) in enumerate(zip(st["new"], st["total"])):
+        numbers = st["block_table"][b, :-(-nk // page)].long()
+        k, v = [_values(codes[numbers].flatten(0, 1)[:nk], scales[numbers].permute(0, 3, 1, 2).flatten(0, 1)[:nk])
+                .transpose(0, 1).contiguous() for codes, scales in ((st["k_cache"], st["k_scale"]), (st["v_cache"], st["v_scale"]))]
+        kt = k.transpose(1, 2).contiguous()                                     # [hkv, 128, nk]
+        rows = max(1, min(nq, (1 << 29) // (hq * nk)))                          # as many queries at a time as 2 GiB of scores hold
+        for r in range(0, nq, rows):
+            n = min(rows, nq - r)
+            q = st["q"][q0 + r:q0 + r + n].float().view(n, hkv, g, DIM).permute(1, 2, 0, 3).reshape(hkv, g * n, DIM)
+            s = torch.matmul(q, kt).mul_(scale).view(hkv, g, n, nk)
+            if case["causal"]:
+                hidden = torch.arange(nk, device=DEV)[None] > (nk - nq + r + torch.arange(n, device=DEV))[:, None]
+                s.masked_fill_(hidden, -math.inf)
+            top = s.amax(dim=-1, keepdim=True)
+            s = s.sub_(top).exp_()
+            den = s.sum(dim=-1, keepdim=True)
+            o = torch.matmul(s.view(hkv, g * n, nk), v).view(hkv, g, n, DIM) / den
+            out[q0 + r:q0 + r + n] = o.permute(2, 0, 1, 3).reshape(n, hq, DIM).to(out.dtype)
+            lse[:, q0 + r:q0 + r + n] = (top + den.log()).view(hq, n)
+        q0 += nq
+    return out, lse
+
+
+# ---- counts and the definition
+
+def work(case):
+    hq, hkv = case["hq"], case["hkv"]
+    new, total = _lengths(case)
+    n = sum(new)
+    if case["op"] == "read":      # codes and scales in, bf16 out
+        return {"bytes": 2.0 * n * hkv * (ROW_BYTES + 2 * DIM), "flops": 2.0 * n * hkv * DIM}
+    if case["op"] == "append":    # bf16 in, codes and scales out, these read back into bf16
+        return {"bytes": 2.0 * n * hkv * (2 * DIM + 2 * ROW_BYTES + 2 * DIM), "flops": 6.0 * n * hkv * DIM}
+    pairs = sum(m * (t - m) + m * (m + 1) // 2 if case["causal"] else m * t for m, t in zip(new, total))
+    return {"bytes": 2.0 * ROW_BYTES * hkv * sum(total) + n * hq * (4.0 * DIM + 4.0), "flops": 4.0 * DIM * hq * pairs}
+
+
+def exact(case, seed):
+    """From the definitions, in 64 bits: every head on its own, pages looked up on the host."""
+    st = prepare(case, seed)
+    f64 = torch.float64
+    page, hq, hkv = case["page"], case["hq"], case["hkv"]
+    table = st["block_table"].tolist()
+
+    def stands_for(codes, scales):      # one byte of codes to two values, sign * (1 or 0).m * 2^e, times 2^(byte - 127)
+        nib = torch.empty(*codes.shape[:-1], DIM, dtype=torch.int64, device=DEV)
+        nib[..., 0::2], nib[..., 1::2] = codes.long() % 16, codes.long() // 16
+        low, up = nib % 2, nib // 2 % 4
+        size = torch.where(up == 0, 0.5 * low.to(f64), (1 + 0.5 * low.to(f64)) * 2.0 ** (up - 1).to(f64))
+        size = torch.where(nib >= 8, -size, size)
+        return size * 2.0 ** (scales.to(f64) - 127).repeat_interleave(GROUP, dim=-1)
+
+    def rounded(x):
+        y = x.to(f64).unflatten(-1, (DIM // GROUP, GROUP))
+        top = y.abs().amax(-1, keepdim=True)
+        e = torch.floor(torch.log2(torch.where(top == 0, torch.ones_like(top), top) * (1 + 1e-12))) - 2      # (bf16: no value is so near above a border)
+        e = e + (top >= 7 * 2.0 ** e)
+        e = torch.where(top == 0, torch.full_like(e, -125), e.clamp(-125, 125))
+        z = y / 2.0 ** e
+        step = torch.where(z.abs() < 2, 0.5, torch.where(z.abs() < 4, 1.0, 2.0)).to(f64)
+        z = torch.round(z / step) * step                                                    # (to even)
+        return (z.clamp(-6, 6) * 2.0 ** e).flatten(-2)
+
+    if case["op"] == "append":
+        return rounded(st["k"]), rounded(st["v"])
+    if case["op"] == "read":
+        where = [(table[b][p // page], p % page) for b, (m, t) in enumerate(zip(st["new"], st["total"])) for p in range(t - m, t)]
+        pages, slots = torch.tensor(where, device=DEV).T
+        return tuple(stands_for(st[c][pages, slots], st[s][pages, :, :, slots]) for c, s in (("k_cache", "k_scale"), ("v_cache", "v_scale")))
+    n = sum(st["new"])
+    out = torch.empty(n, hq, DIM, dtype=f64, device=DEV)
+    lse = torch.empty(hq, n, dtype=f64, device=DEV)
+    q0 = 0
+    for b, (m, t) in enumerate(zip(st["new"], st["total"])):
+        pages = torch.tensor(table[b][:-(-t // page)], device=DEV)
+        for h in range(hkv):
+            k, v = [stands_for(st[c][pages, :, h].reshape(-1, DIM // 2)[:t], st[s][pages, h].transpose(1, 2).reshape(-1, DIM // GROUP)[:t])
+                    for c, s in (("k_cache", "k_scale"), ("v_cache", "v_scale"))]
+            kt = k.t().contiguous()
+            for head in range(h * (hq // hkv), (h + 1) * (hq // hkv)):
+                step = max(1, (1 << 27) // t)
+                for r in range(0, m, step):
+                    e = min(m, r + step)
+                    s = (st["q"][q0 + r:q0 + e, head].to(f64) @ kt) / DIM ** 0.5
+                    if case["causal"]:
+                        last = torch.arange(t - m + r, t - m + e, device=DEV)
+                        s[torch.arange(t, device=DEV)[None, :] > last[:, None]] = -math.inf
+                    lse[head, q0 + r:q0 + e] = torch.logsumexp(s, dim=-1)
+                    out[q0 + r:q0 + e, head] = torch.softmax(s, dim=-1) @ v
+        q0 += m
+    return out, lse
