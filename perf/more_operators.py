@@ -229,22 +229,22 @@ def _run_own(st):
 
     case = st["case"]
     if "handles" not in st:     # made once by a server: the cache, a workspace with room for the chunks' keys
-        cache = pec.PagedCacheFp4(st["k_cache"], st["v_cache"], st["k_scale"], st["v_scale"])
+        cache = pec.PagedCacheMx(st["k_cache"], st["v_cache"], st["k_scale"], st["v_scale"])
         workspace = None
         if case["op"] == "attn":
             chunk_keys = sum(t for m, t in zip(st["new"], st["total"]) if m > case["step_q"]) if case["chunks"] else 0
-            size = pec.pec_paged_fp4_workspace_bytes(case["hq"], case["hkv"], len(st["new"]), sum(st["new"]), chunk_keys)
+            size = pec.pec_paged_mx_workspace_bytes(case["hq"], case["hkv"], len(st["new"]), sum(st["new"]), chunk_keys)
             workspace = torch.empty(size, dtype=torch.uint8, device=DEV)
         st["handles"] = cache, workspace
     cache, workspace = st["handles"]
     if case["op"] == "attn":
-        pec.pec_attn_paged_fp4(st["q"], cache, st["block_table"], st["cu_q"], st["len_k"], max_len_q=max(st["new"]),
+        pec.pec_attn_paged_mx(st["q"], cache, st["block_table"], st["cu_q"], st["len_k"], max_len_q=max(st["new"]),
                                max_len_k=max(st["total"]), causal=case["causal"], out_dtype=st["out"].dtype, out=st["out"],
                                lse=st["lse"], workspace=workspace)
         return st["out"], st["lse"]
     if case["op"] == "append":
-        pec.pec_paged_append_fp4(st["k"], st["v"], cache, st["block_table"], st["cu_q"], st["len_k"])
-    return pec.pec_paged_read_fp4(cache, st["block_table"], st["cu_q"], st["len_k"], k=st["k_out"], v=st["v_out"])
+        pec.pec_paged_append_mx(st["k"], st["v"], cache, st["block_table"], st["cu_q"], st["len_k"])
+    return pec.pec_paged_read_mx(cache, st["block_table"], st["cu_q"], st["len_k"], k=st["k_out"], v=st["v_out"])
 
 
 def _places(st):
