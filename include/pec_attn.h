@@ -403,6 +403,64 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
 size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q);
 
 /*
+ * Keys and values in pages, held in 4 bits: 68 bytes for a head row of 128 in the place of 256.  A value is a sign and one of 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6, times a power of two that 32 neighbouring dims share (the microscaling format with such elements).  Pages and
+ * slots as in pec_paged_cache_t.
+ *   k, v     : DEVICE codes, the 64 bytes of (page, slot, head) at page * page_stride + slot * row_stride + head * head_stride
+ *              (strides in BYTES, multiples of 16, the same for k and v): the code of dim 2 i in the low half of byte i, that of
+ *              dim 2 i + 1 in the high half; sign in bit 3, two bits of exponent, one of fraction.
+ *   k_scale, v_scale: DEVICE scale bytes, that of (page, head, dims 32 g ... 32 g + 31, slot) at page * scale_page_stride + head *
+ *              scale_head_stride + g * page_size + slot (strides in bytes, multiples of 8, the same for both): byte x stands for
+ *              2^(x - 127), 255 for NaN whatever the codes.
+ *   page_size: a power of two from 8 on; a page's slots and heads span less than 2^31 bytes.  No two elements may overlap.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    void* k_scale;
+    void* v_scale;
+    int64_t n_pages;     /* up to 2^31 - 1 */
+    int32_t page_size;
+    int32_t reserved;    /* 0 */
+    int64_t page_stride, row_stride, head_stride;
+    int64_t scale_page_stride, scale_head_stride;
+} pec_paged_cache_mx_t;
+
+/*
+ * New tokens on their way into a paged cache in 4 bits: pec_paged_append with k, after its norm and rotation and one rounding to
+ * bf16, and v rounded to codes.  A group of 32 dims whose largest magnitude is m 2^E, 1 <= m < 2, takes the scale 2^(E - 2), or 2^(E - 1)
+ * where m >= 1.75, kept between 2^-125 and 2^125; values are rounded to the nearest code, ties to the even one, what is beyond 6
+ * to 6.  A group that holds NaN or an infinity is NaN (byte 255, codes 0).  What an element comes back as is off by at most
+ * a fifth of it, or by 0.25 x scale, which is 1/14 of the group's largest magnitude at most.
+ */
+int pec_paged_append_mx(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_mx_t* cache,
+                        const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, void* q_out, void* stream);
+
+/*
+ * Tokens of a paged cache in 4 bits back as packed rows k_out, v_out [total_q, Hkv, 128] bf16, exactly what the codes stand for:
+ * for attention on keys in a row (pec_attn_colocated and the others), or for another GPU.  The batch names the tokens as
+ * pec_paged_append_mx takes them, so the same batch reads what an append has stored, and cu_seqlens_q = the sums of seqlens_k
+ * reads whole sequences.  A token whose position lies in no page or whose page number is outside the cache comes back as zeros; rows
+ * behind the last sequence are left as they were.  Neither output may overlap the cache.  max_len_q and max_len_k do not matter.
+ */
+int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, void* k_out,
+                      void* v_out, void* stream);
+
+/*
+ * pec_attn_paged over a paged cache in 4 bits: the same arguments, masks, empty rows, hidden values, hints and limits; keys and
+ * values are what the codes stand for, exactly.
+ *   workspace: pec_paged_mx_workspace_bytes(shape, batch, total_q, total_k) bytes, 16-byte aligned.  total_k is a number of keys that room
+ *              is made for (512 bytes per key and KV head): sequences with many new tokens have their keys turned into bf16 there, once
+ *              for all of their rows, which is what makes them as fast as on a cache of bf16; those that find no room, and all of
+ *              them with total_k = 0, are worked on straight from the codes, which gives the same results but for rounding and
+ *              takes longer.  Any workspace of at least the size for total_k = 0 will do.
+ */
+int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, const void* q,
+                      int64_t q_stride, int causal, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t pec_paged_mx_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t total_k);
+
+/*
  * On-GPU halves of the head <-> sequence exchange of Ulysses-style sequence parallelism (section
  * "Sequence Parallelism of Megatron and Ulysses": an all-to-all turns "my sequence segment, all
  * heads" into "the whole sequence, my heads" before attention, and back afterwards).  bf16,

@@ -27,6 +27,7 @@ EXPORTS = (
     "pec_sp_workspace_bytes", "pec_sp_prefill_resumable", "pec_sp_resumable_workspace_bytes", "pec_sp_resumable_best_workspace_bytes", "pec_sp_prefill_num_steps", "pec_sp_prefill_step", "pec_decode_splitkv", "pec_ulysses_layout", "pec_sp_select_strategy", "pec_decode_default_splits",
     "pec_decode_workspace_bytes", "pec_decode_splitkv_static", "pec_mfma_probe", "pec_hbm_read_probe", "pec_attn_colocated", "pec_colocated_workspace_bytes", "pec_attn_varlen", "pec_varlen_workspace_bytes", "pec_status_string",
     "pec_qk_norm_rope", "pec_paged_append", "pec_attn_paged", "pec_paged_workspace_bytes",
+    "pec_paged_append_mx", "pec_paged_read_mx", "pec_attn_paged_mx", "pec_paged_mx_workspace_bytes",
 )
 
 
@@ -52,6 +53,13 @@ class PecPagedCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
+
+
+class PecPagedCacheMx(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("scale_page_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
 
 
 class PecPagedBatch(ctypes.Structure):
@@ -125,6 +133,15 @@ def lib() -> ctypes.CDLL:
         L.pec_attn_paged.restype = ci
         L.pec_paged_workspace_bytes.argtypes = [sp, i32, i64]
         L.pec_paged_workspace_bytes.restype = sz
+        pm = ctypes.POINTER(PecPagedCacheMx)
+        L.pec_paged_append_mx.argtypes = [sp, nr, pm, pb, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.pec_paged_append_mx.restype = ci
+        L.pec_paged_read_mx.argtypes = [sp, pm, pb, vp, vp, vp]
+        L.pec_paged_read_mx.restype = ci
+        L.pec_attn_paged_mx.argtypes = [sp, pm, pb, vp, i64, ci, vp, vp, vp, sz, vp]
+        L.pec_attn_paged_mx.restype = ci
+        L.pec_paged_mx_workspace_bytes.argtypes = [sp, i32, i64, i64]
+        L.pec_paged_mx_workspace_bytes.restype = sz
         L.pec_hbm_read_probe.argtypes = [vp, sz, vp, vp]
         L.pec_hbm_read_probe.restype = ci
         L.pec_mfma_probe.argtypes = [vp, sz, i32, vp, sz, vp]
@@ -490,6 +507,29 @@ class PagedCache:
         self.ref = ctypes.byref(self.struct)
 
 
+class PagedCacheMx:
+    """A server's key / value pages held in 4 bits, laid out once: k, v uint8 [n_pages, page_size, Hkv, 64], two codes a byte, with a
+    contiguous last dim and any other strides (multiples of 16; a cache laid out by heads is passed as its transpose(1, 2)); k_scale,
+    v_scale uint8 [n_pages, Hkv, 4, page_size], a byte for 32 dims, their last two dims contiguous.  All on one GPU, k and v with the same strides."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        for t, n in ((k, "k"), (v, "v")):
+            if not (t.is_cuda and t.dtype == torch.uint8 and t.dim() == 4 and t.shape[3] == 64 and t.stride(3) == 1):
+                raise ValueError("%s must be a uint8 tensor [n_pages, page_size, heads, 64] on the GPU, its last dim contiguous" % n)
+        if k.shape != v.shape or k.stride() != v.stride() or k.device != v.device:
+            raise ValueError("k and v must have the same shape and strides, on the same GPU")
+        n_pages, page, heads, _ = k.shape
+        for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.uint8 or t.shape != (n_pages, heads, 4, page) or t.stride()[2:] != (page, 1) or t.device != k.device:
+                raise ValueError("%s must be a uint8 tensor [n_pages, heads, 4, page_size], its last two dims contiguous, on the GPU of k" % n)
+        if k_scale.stride() != v_scale.stride():
+            raise ValueError("k_scale and v_scale must have the same strides")
+        self.k, self.v, self.k_scale, self.v_scale, self.index, self.n_kv_heads = k, v, k_scale, v_scale, k.get_device(), heads
+        self.struct = PecPagedCacheMx(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages, page, 0,
+                                      k.stride(0), k.stride(1), k.stride(2), k_scale.stride(0), k_scale.stride(1))
+        self.ref = ctypes.byref(self.struct)
+
+
 class NormRope:
     """What a model does to its query and key rows: norm weights (fp32 [128] or None) and the rotation's angles (cos_sin fp32
     [n_positions, R], the R / 2 cosines of a position, then its sines; None: no rotation)."""
@@ -600,11 +640,7 @@ def pec_qk_norm_rope(q, k, norm_rope: NormRope, positions=None, pos0: int = 0, q
     return q_out, k_out
 
 
-def pec_paged_append(k, v, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, norm_rope: NormRope = None, q=None, q_out=None,
-                     stream=None):
-    """The new tokens' k (normed and rotated), v [T,Hkv,128] into their sequences' pages; q [T,Hq,128], if given, normed and
-    rotated into q_out, which is returned.  cu_seqlens_q [B+1], seqlens_k [B] (the new tokens among them) and block_table
-    [B, pages], all int32 on the GPU."""
+def _append(fn, name, k, v, cache, block_table, cu_seqlens_q, seqlens_k, norm_rope, q, q_out, stream):
     index, sizes = cache.index, k.shape
     k_stride, v_stride = _rows(k, "k", index), _rows(v, "v", index)
     tokens, hkv = sizes[0], sizes[1]
@@ -625,9 +661,17 @@ def pec_paged_append(k, v, cache: PagedCache, block_table, cu_seqlens_q, seqlens
         if norm_rope.index not in (None, index):
             raise ValueError("norm_rope is on another GPU")
     batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, tokens, 0, 0, index)
-    _call(lib().pec_paged_append, "pec_paged_append", index, stream, _shape_ref(hq, hkv, _BF16, 0.0, 0), turn, cache.ref, batch, q_at,
-          q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, qo_at)
+    _call(fn, name, index, stream, _shape_ref(hq, hkv, _BF16, 0.0, 0), turn, cache.ref, batch, q_at, q_stride,
+          k.data_ptr(), k_stride, v.data_ptr(), v_stride, qo_at)
     return q_out
+
+
+def pec_paged_append(k, v, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, norm_rope: NormRope = None, q=None, q_out=None,
+                     stream=None):
+    """The new tokens' k (normed and rotated), v [T,Hkv,128] into their sequences' pages; q [T,Hq,128], if given, normed and
+    rotated into q_out, which is returned.  cu_seqlens_q [B+1], seqlens_k [B] (the new tokens among them) and block_table
+    [B, pages], all int32 on the GPU."""
+    return _append(lib().pec_paged_append, "pec_paged_append", k, v, cache, block_table, cu_seqlens_q, seqlens_k, norm_rope, q, q_out, stream)
 
 
 def pec_paged_workspace_bytes(n_q_heads: int, n_kv_heads: int, batch: int, total_q: int) -> int:
@@ -654,4 +698,58 @@ def pec_attn_paged(q, cache: PagedCache, block_table, cu_seqlens_q, seqlens_k, m
         workspace = _empty(max(16, n), _U8, q.device, stream, result=False)
     _call(lib().pec_attn_paged, "pec_attn_paged", index, stream, shp, cache.ref, batch, q.data_ptr(), q_stride, 1 if causal else 0, out_at,
           lse_at, _on(workspace, _U8, "workspace", index), workspace.numel())
+    return out, lse
+
+
+# ---- keys and values in pages, held in 4 bits
+
+def pec_paged_append_mx(k, v, cache: PagedCacheMx, block_table, cu_seqlens_q, seqlens_k, norm_rope: NormRope = None, q=None, q_out=None,
+                        stream=None):
+    """pec_paged_append into a cache in 4 bits: k (normed, rotated and rounded to bf16) and v are rounded to codes on their way."""
+    return _append(lib().pec_paged_append_mx, "pec_paged_append_mx", k, v, cache, block_table, cu_seqlens_q, seqlens_k, norm_rope, q, q_out,
+                   stream)
+
+
+def pec_paged_read_mx(cache: PagedCacheMx, block_table, cu_seqlens_q, seqlens_k, total_q: int = None, k=None, v=None, stream=None):
+    """The batch's tokens (as pec_paged_append_mx takes them) back from the cache -> (k, v) [T,Hkv,128] bf16.  T is total_q, or the rows of
+    the tensors given for the results."""
+    index, given = cache.index, k if k is not None else v
+    if given is None and total_q is None:
+        raise ValueError("total_q, or a tensor for the results")
+    shape = (given.shape[0] if total_q is None else int(total_q), cache.n_kv_heads, 128)
+    if k is None:
+        k = _empty(shape, _BF16, cache.k.device, stream)
+    if v is None:
+        v = _empty(shape, _BF16, cache.k.device, stream)
+    k_at, v_at = _on(k, _BF16, "k", index, shape), _on(v, _BF16, "v", index, shape)
+    batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, shape[0], 0, 0, index)
+    _call(lib().pec_paged_read_mx, "pec_paged_read_mx", index, stream, _shape_ref(shape[1], shape[1], _BF16, 0.0, 0), cache.ref, batch,
+          k_at, v_at)
+    return k, v
+
+
+def pec_paged_mx_workspace_bytes(n_q_heads: int, n_kv_heads: int, batch: int, total_q: int, total_k: int = 0) -> int:
+    """total_k: keys of sequences with many new tokens that room is made for (see pec_attn.h)."""
+    return int(lib().pec_paged_mx_workspace_bytes(_shape_ref(n_q_heads, n_kv_heads, _BF16, 0.0, 0), int(batch), int(total_q), int(total_k)))
+
+
+def pec_attn_paged_mx(q, cache: PagedCacheMx, block_table, cu_seqlens_q, seqlens_k, max_len_q: int = 0, max_len_k: int = 0,
+                      causal: bool = True, out_dtype=torch.bfloat16, scale: float = 0.0, flags: int = 0, out=None, lse=None,
+                      workspace=None, total_k: int = 0, stream=None):
+    """pec_attn_paged over a cache in 4 bits.  total_k: keys that a workspace made here has room for (see pec_paged_mx_workspace_bytes)."""
+    index, sizes = cache.index, q.shape
+    q_stride = _rows(q, "q", index)
+    total, hq = sizes[0], sizes[1]
+    if out is None:
+        out = _empty(sizes, out_dtype, q.device, stream)
+    if lse is None:
+        lse = _empty((hq, total), _F32, q.device, stream)
+    out_at, lse_at = _on(out, out_dtype, "out", index, sizes), _on(lse, _F32, "lse", index, (hq, total))
+    batch = _paged_batch(block_table, cu_seqlens_q, seqlens_k, total, max_len_q, max_len_k, index)
+    shp = _shape_ref(hq, cache.n_kv_heads, out_dtype, float(scale), int(flags))
+    if workspace is None:
+        n = int(lib().pec_paged_mx_workspace_bytes(shp, seqlens_k.numel(), total, int(total_k)))
+        workspace = _empty(max(16, n), _U8, q.device, stream, result=False)
+    _call(lib().pec_attn_paged_mx, "pec_attn_paged_mx", index, stream, shp, cache.ref, batch, q.data_ptr(), q_stride, 1 if causal else 0,
+          out_at, lse_at, _on(workspace, _U8, "workspace", index), workspace.numel())
     return out, lse

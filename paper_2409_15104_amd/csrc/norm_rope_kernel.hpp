@@ -17,6 +17,7 @@
 #include <stdint.h>
 
 #include "paged_common.hpp"
+#include "paged_mx_common.hpp"
 
 namespace pec {
 
@@ -32,8 +33,11 @@ struct NormRopeParams {
     float eps;
     int32_t tokens, n_q_heads, n_kv_heads;   // n_q_heads 0: no queries
     int32_t parts;                           // wavefronts per token
-    PagedKv cache;                           // append only
+    PagedKv cache;                           // append only; of a cache in 4 bits the codes
     PagedBatch batch;
+    unsigned char *k_scale, *v_scale;        // append to a cache in 4 bits only, as in PagedMx
+    int64_t scale_page_b;
+    uint32_t scale_head_b;
 };
 
 constexpr int kNormRopeThreads = 256;
@@ -50,9 +54,12 @@ __device__ __forceinline__ float row_rotated(float x, int ctrl) {     // 16 lane
 // PAIRS: which values a rotation combines: kPairsNone, kPairsFar (i, i + 64), kPairsHalf (i, i + R / 2) of any R, kPairsNext
 // (2 i, 2 i + 1).
 enum { kPairsNone = 0, kPairsFar = 1, kPairsHalf = 2, kPairsNext = 3 };
+// TO: where the keys go, and the values with them: packed rows (no values), a paged cache, a paged cache in 4 bits.
+enum { kToRows = 0, kToPages = 1, kToMxPages = 2 };
 
-template <bool NORM, int PAIRS, bool APPEND>
+template <bool NORM, int PAIRS, int TO>
 __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormRopeParams p) {
+    constexpr bool APPEND = TO != kToRows, MX = TO == kToMxPages;
     const int lane = threadIdx.x & 63, c = lane & 15, sub = lane >> 4;
     const int64_t w = ((int64_t)blockIdx.y * kNormRopeRow + blockIdx.x) * (kNormRopeThreads / 64) +
                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -82,6 +89,7 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
     // ---- the token's position, and its place in the cache
     int64_t at;
     unsigned char *k_slot = nullptr, *v_slot = nullptr;      // null: no place for it
+    [[maybe_unused]] int64_t scale_off = 0;
     if constexpr (APPEND) {
         const int b = __builtin_amdgcn_readfirstlane(paged_owner(p.batch, token));
         if (b < 0) return;                                   // a row behind the last sequence
@@ -93,6 +101,7 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                 const int64_t off = number * p.cache.page_b + (at & ((1 << p.cache.log_page) - 1)) * (int64_t)p.cache.row_b;
                 k_slot = p.cache.k + off;
                 v_slot = p.cache.v + off;
+                if constexpr (MX) scale_off = number * p.scale_page_b + (at & ((1 << p.cache.log_page) - 1)) + ((c >> 2) << p.cache.log_page);
             }
         }
     } else {
@@ -217,6 +226,15 @@ __global__ __launch_bounds__(kNormRopeThreads) void norm_rope_kernel(const NormR
                 *reinterpret_cast<u32x4*>(p.q_out + ((int64_t)token * p.n_q_heads + head) * kHeadDim + 8 * c) = y;
             } else if (!APPEND) {
                 *reinterpret_cast<u32x4*>(p.k_out + ((int64_t)token * p.n_kv_heads + head) * kHeadDim + 8 * c) = y;
+            } else if constexpr (MX) {
+                // (keys are rounded to bf16 before: what is held is what a cache of bf16 would be rounded to, whether a call
+                // norms and rotates or pec_qk_norm_rope has done so)
+                unsigned char* const slot = kind == K ? k_slot : v_slot;
+                const uint32_t byte = mx_scale_byte(mx_top_of_group(y));
+                if (slot) {
+                    *reinterpret_cast<uint32_t*>(slot + (int64_t)head * p.cache.head_b + 4 * c) = mx_codes(y, byte);
+                    if ((c & 3) == 0) (kind == K ? p.k_scale : p.v_scale)[scale_off + (int64_t)head * p.scale_head_b] = (unsigned char)byte;
+                }
             } else {
                 unsigned char* const slot = kind == K ? k_slot : v_slot;
                 if (slot) *reinterpret_cast<u32x4*>(slot + (int64_t)head * p.cache.head_b + 16 * c) = y;

@@ -95,30 +95,55 @@ int check_norm_rope(const pec_norm_rope_t* n, NormRopeParams* p) {
     return PEC_OK;
 }
 
-template <bool NORM, bool APPEND>
+template <bool NORM, int TO>
 void launch_norm_rope(const NormRopeParams& p, dim3 grid, hipStream_t st) {
     const dim3 threads(kNormRopeThreads);
     if (p.rotary == 0)
-        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNone, APPEND>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNone, TO>), grid, threads, 0, st, p);
     else if (p.interleaved)
-        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNext, APPEND>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsNext, TO>), grid, threads, 0, st, p);
     else if (p.rotary == kHeadDim)
-        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsFar, APPEND>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsFar, TO>), grid, threads, 0, st, p);
     else
-        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsHalf, APPEND>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((norm_rope_kernel<NORM, kPairsHalf, TO>), grid, threads, 0, st, p);
 }
 
-int launch_norm_rope(NormRopeParams& p, bool append, hipStream_t st) {
-    p.parts = norm_rope_parts(compute_units(), p.tokens, (p.n_q_heads + 3) / 4 + (append ? 2 : 1) * ((p.n_kv_heads + 3) / 4));
+int launch_norm_rope(NormRopeParams& p, int to, hipStream_t st) {
+    p.parts = norm_rope_parts(compute_units(), p.tokens, (p.n_q_heads + 3) / 4 + (to != kToRows ? 2 : 1) * ((p.n_kv_heads + 3) / 4));
     const int64_t waves = (int64_t)p.tokens * p.parts;
     const int64_t blocks = (waves + kNormRopeThreads / 64 - 1) / (kNormRopeThreads / 64);
     const dim3 grid((unsigned)std::min<int64_t>(blocks, kNormRopeRow), (unsigned)((blocks + kNormRopeRow - 1) / kNormRopeRow));
     const bool norm = p.q_weight || p.k_weight;
-    if (append && norm) launch_norm_rope<true, true>(p, grid, st);
-    else if (append) launch_norm_rope<false, true>(p, grid, st);
-    else if (norm) launch_norm_rope<true, false>(p, grid, st);
-    else launch_norm_rope<false, false>(p, grid, st);
+    if (to == kToMxPages && norm) launch_norm_rope<true, kToMxPages>(p, grid, st);
+    else if (to == kToMxPages) launch_norm_rope<false, kToMxPages>(p, grid, st);
+    else if (to == kToPages && norm) launch_norm_rope<true, kToPages>(p, grid, st);
+    else if (to == kToPages) launch_norm_rope<false, kToPages>(p, grid, st);
+    else if (norm) launch_norm_rope<true, kToRows>(p, grid, st);
+    else launch_norm_rope<false, kToRows>(p, grid, st);
     return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
+
+// An append whose cache has been checked.
+int append_call(NormRopeParams& p, int to, int page_size, const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
+                const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                int64_t v_stride, void* q_out, void* stream) {
+    if (int rc = check_batch(batch, page_size, &p.batch)) return rc;
+    if (int rc = check_norm_rope(norm_rope, &p)) return rc;
+    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
+    if (!k || !v || (q && !q_out)) return PEC_ERR_INVALID_ARGUMENT;
+    p.q_stride = token_stride(q_stride, shape->n_q_heads);
+    p.k_stride = token_stride(k_stride, shape->n_kv_heads);
+    p.v_stride = token_stride(v_stride, shape->n_kv_heads);
+    if ((q && p.q_stride < 0) || p.k_stride < 0 || p.v_stride < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_out)) return PEC_ERR_MISALIGNED;
+    p.q = static_cast<const __bf16*>(q);
+    p.k = static_cast<const __bf16*>(k);
+    p.v = static_cast<const __bf16*>(v);
+    p.q_out = static_cast<__bf16*>(q_out);
+    p.tokens = (int32_t)batch->total_q;
+    p.n_q_heads = q ? shape->n_q_heads : 0;
+    p.n_kv_heads = shape->n_kv_heads;
+    return launch_norm_rope(p, to, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace
@@ -151,7 +176,7 @@ int pec_qk_norm_rope(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
     p.tokens = (int32_t)tokens;
     p.n_q_heads = q ? shape->n_q_heads : 0;
     p.n_kv_heads = k ? shape->n_kv_heads : 0;
-    return launch_norm_rope(p, false, static_cast<hipStream_t>(stream));
+    return launch_norm_rope(p, kToRows, static_cast<hipStream_t>(stream));
 }
 
 int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_t* cache,
@@ -161,23 +186,7 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
     if (shape->flags != 0) return PEC_ERR_UNSUPPORTED;
     NormRopeParams p{};
     if (int rc = check_cache(shape, cache, &p.cache)) return rc;
-    if (int rc = check_batch(batch, cache->page_size, &p.batch)) return rc;
-    if (int rc = check_norm_rope(norm_rope, &p)) return rc;
-    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
-    if (!k || !v || (q && !q_out)) return PEC_ERR_INVALID_ARGUMENT;
-    p.q_stride = token_stride(q_stride, shape->n_q_heads);
-    p.k_stride = token_stride(k_stride, shape->n_kv_heads);
-    p.v_stride = token_stride(v_stride, shape->n_kv_heads);
-    if ((q && p.q_stride < 0) || p.k_stride < 0 || p.v_stride < 0) return PEC_ERR_INVALID_ARGUMENT;
-    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_out)) return PEC_ERR_MISALIGNED;
-    p.q = static_cast<const __bf16*>(q);
-    p.k = static_cast<const __bf16*>(k);
-    p.v = static_cast<const __bf16*>(v);
-    p.q_out = static_cast<__bf16*>(q_out);
-    p.tokens = (int32_t)batch->total_q;
-    p.n_q_heads = q ? shape->n_q_heads : 0;
-    p.n_kv_heads = shape->n_kv_heads;
-    return launch_norm_rope(p, true, static_cast<hipStream_t>(stream));
+    return append_call(p, kToPages, cache->page_size, shape, norm_rope, batch, q, q_stride, k, k_stride, v, v_stride, q_out, stream);
 }
 
 size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q) {

@@ -1,0 +1,123 @@
+// C-ABI host side of the paged cache in 4 bits: argument validation and launches of pec_paged_append_mx, pec_paged_read_mx and
+// pec_attn_paged_mx.  Part of pec_attn.hip.
+#pragma once
+
+namespace {
+
+int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx* out) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || c->n_pages <= 0 || c->page_size <= 0 || c->reserved != 0)
+        return PEC_ERR_INVALID_ARGUMENT;
+    if (c->page_size < 8 || (c->page_size & (c->page_size - 1)) != 0 || c->n_pages > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
+    if (misaligned(c->k) || misaligned(c->v) || misaligned(c->k_scale) || misaligned(c->v_scale) ||
+        ((c->page_stride | c->row_stride | c->head_stride) & 15) || ((c->scale_page_stride | c->scale_head_stride) & 7))
+        return PEC_ERR_MISALIGNED;
+    const int64_t most = (int64_t)1 << 31, most_page = (int64_t)1 << 46, scales = (int64_t)c->page_size * kMxGroups;      // bytes
+    const bool heads = s->n_kv_heads > 1, pages = c->n_pages > 1;
+    if (c->row_stride < kMxRowBytes || c->row_stride > most || (heads && (c->head_stride < kMxRowBytes || c->head_stride > most)) ||
+        (heads && (c->scale_head_stride < scales || c->scale_head_stride > most)) || c->page_stride < 0 || c->page_stride > most_page ||
+        c->scale_page_stride < 0 || c->scale_page_stride > most_page || (pages && (c->page_stride < kMxRowBytes || c->scale_page_stride < scales)))
+        return PEC_ERR_INVALID_ARGUMENT;
+    const int64_t head_stride = heads ? c->head_stride : 0, scale_head_stride = heads ? c->scale_head_stride : 0;
+    if ((c->page_size - 1) * c->row_stride + (s->n_kv_heads - 1) * head_stride + kMxRowBytes > most - 16 ||
+        (s->n_kv_heads - 1) * scale_head_stride + scales > most - 16)
+        return PEC_ERR_UNSUPPORTED;
+    out->k = static_cast<unsigned char*>(c->k);
+    out->v = static_cast<unsigned char*>(c->v);
+    out->ks = static_cast<unsigned char*>(c->k_scale);
+    out->vs = static_cast<unsigned char*>(c->v_scale);
+    out->page_b = c->page_stride;
+    out->scale_page_b = c->scale_page_stride;
+    out->row_b = (uint32_t)c->row_stride;
+    out->head_b = (uint32_t)head_stride;
+    out->scale_head_b = (uint32_t)scale_head_stride;
+    out->last_page = (uint32_t)(c->n_pages - 1);
+    out->log_page = 0;
+    while ((1 << out->log_page) < c->page_size) ++out->log_page;
+    return PEC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pec_paged_append_mx(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_mx_t* cache,
+                        const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, void* q_out, void* stream) {
+    if (int rc = check_shape(shape, nullptr)) return rc;
+    if (shape->flags != 0) return PEC_ERR_UNSUPPORTED;
+    NormRopeParams p{};
+    PagedMx c;
+    if (int rc = check_cache_mx(shape, cache, &c)) return rc;
+    p.cache.k = c.k;
+    p.cache.v = c.v;
+    p.cache.page_b = c.page_b;
+    p.cache.row_b = c.row_b;
+    p.cache.head_b = c.head_b;
+    p.cache.last_page = c.last_page;
+    p.cache.log_page = c.log_page;
+    p.k_scale = c.ks;
+    p.v_scale = c.vs;
+    p.scale_page_b = c.scale_page_b;
+    p.scale_head_b = c.scale_head_b;
+    return append_call(p, kToMxPages, cache->page_size, shape, norm_rope, batch, q, q_stride, k, k_stride, v, v_stride, q_out, stream);
+}
+
+int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, void* k_out,
+                      void* v_out, void* stream) {
+    if (int rc = check_shape(shape, nullptr)) return rc;
+    if (shape->flags != 0) return PEC_ERR_UNSUPPORTED;
+    PagedMxReadParams p{};
+    if (int rc = check_cache_mx(shape, cache, &p.cache)) return rc;
+    if (int rc = check_batch(batch, cache->page_size, &p.batch)) return rc;
+    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
+    if (!k_out || !v_out) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(k_out) || misaligned(v_out)) return PEC_ERR_MISALIGNED;
+    p.k_out = static_cast<__bf16*>(k_out);
+    p.v_out = static_cast<__bf16*>(v_out);
+    p.n_kv_heads = shape->n_kv_heads;
+    const int64_t groups = (batch->total_q + 3) / 4;
+    p.parts = norm_rope_parts(compute_units(), groups, 2 * (int64_t)p.n_kv_heads);
+    const int64_t blocks = (groups * p.parts + 3) / 4;
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, kMxReadRow), (unsigned)((blocks + kMxReadRow - 1) / kMxReadRow));
+    hipLaunchKernelGGL(paged_mx_read_kernel, grid, dim3(256), 0, static_cast<hipStream_t>(stream), p);
+    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
+
+size_t pec_paged_mx_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t total_k) {
+    if (total_k < 0) return 0;
+    return pec_paged_workspace_bytes(shape, batch, total_q);
+}
+
+int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, const void* q,
+                      int64_t q_stride, int causal, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    float scale;
+    if (int rc = check_shape(shape, &scale)) return rc;
+    if (shape->flags & ~(uint32_t)PEC_FLAG_SIMPLE_KERNEL) return PEC_ERR_UNSUPPORTED;
+    PagedAttnParams p{};
+    PagedMx mx;
+    if (int rc = check_cache_mx(shape, cache, &mx)) return rc;
+    if (int rc = check_batch(batch, cache->page_size, &p.batch)) return rc;
+    if (batch->batch == 0 || batch->total_q == 0) return PEC_OK;
+    if (!q || !out || !lse) return PEC_ERR_INVALID_ARGUMENT;
+    p.q_stride = token_stride(q_stride, shape->n_q_heads);
+    if (p.q_stride < 0) return PEC_ERR_INVALID_ARGUMENT;
+    if (misaligned(q) || misaligned(out) || misaligned(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return PEC_ERR_MISALIGNED;
+    const bool simple = (shape->flags & PEC_FLAG_SIMPLE_KERNEL) != 0;
+    if (!simple && (!workspace || workspace_bytes < pec_paged_mx_workspace_bytes(shape, batch->batch, batch->total_q, 0))) return PEC_ERR_WORKSPACE;
+    p.q = static_cast<const __bf16*>(q);
+    p.out = out;
+    p.lse = lse;
+    p.n_q_heads = shape->n_q_heads;
+    p.n_kv_heads = shape->n_kv_heads;
+    p.group = shape->n_q_heads / shape->n_kv_heads;
+    p.causal = causal != 0;
+    p.out_f32 = shape->out_dtype == PEC_F32;
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t rows = batch->total_q * shape->n_q_heads;
+    hipLaunchKernelGGL(paged_mx_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p, mx);
+    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
+
+}  // extern "C"

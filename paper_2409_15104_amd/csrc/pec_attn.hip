@@ -24,6 +24,9 @@
 #include "kernel_choice.hpp"
 #include "norm_rope_kernel.hpp"
 #include "paged_list.hpp"
+#include "paged_mx_common.hpp"
+#include "paged_mx_read_kernel.hpp"
+#include "paged_mx_simple_kernel.hpp"
 #include "paged_simple_kernel.hpp"
 #include "paged_step_kernel.hpp"
 #include "probes.hpp"
@@ -934,3 +937,4 @@ const char* pec_status_string(int status) {
 }  // extern "C"
 
 #include "paged_calls.hpp"
+#include "paged_mx_calls.hpp"
