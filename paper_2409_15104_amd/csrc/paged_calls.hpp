@@ -146,6 +146,22 @@ int append_call(NormRopeParams& p, int to, int page_size, const pec_shape_t* sha
     return launch_norm_rope(p, to, static_cast<hipStream_t>(stream));
 }
 
+// The merge of spans' pieces: `tokens` workgroups for every sequence and query head.
+void launch_paged_merge(const PagedStepParams& s, int cu, int tokens, int64_t len_k, hipStream_t st) {
+    const int batch = s.a.batch.batch;
+    const int64_t rows = (int64_t)batch * tokens, waves_wanted = (int64_t)cu * 8;
+    const unsigned heads = (unsigned)s.a.n_q_heads;
+    // pieces of the longest unit, as far as the hints tell: a step each at most, and four times a sequence's share of the spans
+    const int64_t pieces = std::min({len_k / kStepTile, (int64_t)s.n_spans.d, 4 * (int64_t)s.n_spans.d / batch});
+    if (rows * heads >= waves_wanted)
+        hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), heads), dim3(256), 0, st, s,
+                           tokens);
+    else if (pieces < 128 || rows * heads > 512)
+        hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, heads), dim3(256), 0, st, s, tokens);
+    else
+        hipLaunchKernelGGL(paged_merge_kernel<16>, dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
+}
+
 }  // namespace
 
 extern "C" {
@@ -271,17 +287,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
         // (beside a list most of these sequences are decode steps; the tokens of others are merged one after the other)
         const int tokens = cut.list ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256));
-        const int64_t rows = (int64_t)batch->batch * tokens, waves_wanted = (int64_t)cu * 8;
-        const unsigned heads = (unsigned)shape->n_q_heads;
-        // pieces of the longest unit, as far as the hints tell: a step each at most, and four times a sequence's share of the spans
-        const int64_t pieces = std::min({len_k / kStepTile, (int64_t)s.n_spans.d, 4 * (int64_t)s.n_spans.d / batch->batch});
-        if (rows * heads >= waves_wanted)
-            hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), heads), dim3(256), 0, st, s,
-                               tokens);
-        else if (pieces < 128 || rows * heads > 512)
-            hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, heads), dim3(256), 0, st, s, tokens);
-        else
-            hipLaunchKernelGGL(paged_merge_kernel<16>, dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
+        launch_paged_merge(s, cu, tokens, len_k, st);
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     }
     if (!cut.list) return PEC_OK;

@@ -36,6 +36,10 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
     return PEC_OK;
 }
 
+// Of row tiles of 16 that a wavefront of paged_mx_step_kernel takes, for sequences of up to so many rows; wavefronts per workgroup.
+int mx_step_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+constexpr int mx_step_waves(int nt) { return nt == 4 ? 4 : 8; }
+
 }  // namespace
 
 extern "C" {
@@ -115,8 +119,50 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t rows = batch->total_q * shape->n_q_heads;
-    hipLaunchKernelGGL(paged_mx_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p, mx);
+    if (simple) {
+        const int64_t rows = batch->total_q * shape->n_q_heads;
+        hipLaunchKernelGGL(paged_mx_simple_kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(64), 0, st, p, mx);
+        return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    }
+    if (batch->batch > kPagedChunks * 64) return PEC_ERR_UNSUPPORTED;
+    const int cu = std::max(8, compute_units() & ~7), g = p.group;
+    if (batch->total_q * g > 0x7fffffff - 64) return PEC_ERR_UNSUPPORTED;      // rows of a KV head
+    const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
+    const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
+    char* const ws = static_cast<char*>(workspace);
+    const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
+    // offsets of the last page's last element, from a head's first one
+    const int64_t furthest = (int64_t)mx.last_page * mx.page_b + (int64_t)cache->page_size * mx.row_b,
+                  furthest_scale = (int64_t)mx.last_page * mx.scale_page_b + (int64_t)cache->page_size * kMxGroups;
+    const bool wide = std::max(furthest, furthest_scale) > 0xffffffffll;
+    PagedStepParams s{};
+    s.a = p;
+    const int nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
+    s.part_out = reinterpret_cast<float*>(ws);
+    s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+    s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
+    s.cut = StepCut{fast_div(g), nt == 1 ? 4 : nt == 2 ? 5 : 6, p.causal, 0x7fffffff};
+    const int waves = cu * waves_per;
+    if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
+    s.n_spans = fast_div(waves / p.n_kv_heads);
+    s.kv_heads = fast_div(p.n_kv_heads);
+    s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
+    const int64_t row_tiles = batch->total_q * g / (16 * nt) + batch->batch;
+    if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
+    const dim3 grid((unsigned)cu), threads((unsigned)waves_per * 64);
+    auto launch = [&](auto tiles, auto is_wide) {
+        constexpr int NT = decltype(tiles)::value;
+        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), 2, false, decltype(is_wide)::value>), grid, threads, 0, st, s, mx);
+    };
+    auto launch_nt = [&](auto is_wide) {
+        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_wide);
+        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_wide);
+        else launch(std::integral_constant<int, 4>{}, is_wide);
+    };
+    if (wide) launch_nt(std::true_type{});
+    else launch_nt(std::false_type{});
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
     return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
 }
 

@@ -1,0 +1,519 @@
+// Attention over a paged cache in 4 bits for sequences with few new tokens: decode steps, drafted tokens, short chunks (gfx950).
+//
+// The work is shared out as in paged_step_kernel: units of up to R query rows that share a KV head, a line of 32-key tiles for each
+// KV head cut into equal spans, one for every wavefront of the chip, pieces merged by paged_merge_kernel; or, for small calls, a
+// workgroup per unit.  What differs is the tile.  In 4 bits it is 4.25 KiB in the place of 16, so it goes from memory straight to
+// registers, S tiles ahead, with no LDS and no wait but the compiler's; and since a byte now stands for two values, what a
+// wavefront does per byte counts four times as much as there.
+//
+// Products are 16 x 16 x 32 (lane l: m = l % 16, c = l / 16; A rows m, B columns m, k-slots 8 c ... 8 c + 7; C column m, rows 4 c + i).
+// Scores, S^T = K Q^T: the contraction runs over dims in any order that K and Q agree on, so lane (m, c) takes dims 32 c ... 32 c + 31
+// of a key, 16 bytes of codes in one load and exactly one scale group, eight dims for each of four products.  Row 4 c + i of product u is
+// key 8 c + 4 u + i, so that lane c ends up with the scores of the eight keys 8 c ... 8 c + 7, which is the order in which
+// O^T += V^T P^T wants them.  There row m of block j is dim 8 m + j: a lane needs of each of its eight keys the four bytes of dims
+// 8 m ... 8 m + 7, converts them in pairs of dims and exchanges halves between neighbouring keys, two instructions for two values.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "paged_mx_common.hpp"
+#include "paged_step_kernel.hpp"
+
+namespace pec {
+
+// Steps that a span should have at least, as least_span(), a step taking its wavefront 0.6 us.
+__device__ __forceinline__ int least_span_mx(int total, int longest, int n_kv_heads, int unit_rows) {
+    const float merge_us = (float)longest * (1.f / 128.f) + (float)total * (float)(n_kv_heads * unit_rows) * (1.f / 3900.f);
+    return max(1, (int)__builtin_amdgcn_sqrtf(merge_us * (1.f / 0.6f)));
+}
+
+struct MxTile {              // 32 keys, as lane (m, c) takes them
+    u32x4 k[2];              // dims 32 c ... 32 c + 31 of keys 8 (m / 4) + 4 u + m % 4
+    uint32_t v[8];           // dims 8 m ... 8 m + 7 of keys 8 c + e
+    u32x2 ks, vs;            // scale bytes of keys 8 (m / 4) ... + 7 for group c, of keys 8 c ... + 7 for group m / 4
+};
+
+// WIDE: offsets in the cache need more than 32 bits.
+template <int NT, int WAVES, int S, bool SHARED, bool WIDE>
+__global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const PagedStepParams p, const PagedMx cache) {
+    constexpr int R = 16 * NT;
+    constexpr int STRIDE = SHARED ? WAVES : 1;
+    using Off = std::conditional_t<WIDE, uint64_t, uint32_t>;
+    __shared__ __attribute__((aligned(1024))) float joint_o[SHARED ? WAVES * 16 * kHeadDim : 1];
+    __shared__ float joint[SHARED ? 3 * WAVES * 16 : 1];
+    __shared__ int32_t chunk_sum[kPagedChunks];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, m = lane & 15, c = lane >> 4;
+    const int g = p.a.group, causal = p.a.causal;
+    const StepCut& cut = p.cut;
+    const PagedBatch& bt = p.a.batch;
+
+    auto length = [&](const PagedSeq& s) { return SHARED ? cut.row_tiles(s) : cut.all_tiles(s); };
+    PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
+    if (!SHARED && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
+        for (int ch = wave, ahead = 0, at = 0; ch < line.n_chunks; ch += WAVES) {
+            for (; at < ch; ++at) ahead = add_up(ahead, chunk_sum[at]);
+            const int mine = length(line.load(64 * ch + lane)), all = wave_prefix(mine);
+            if (64 * ch + lane < bt.batch) p.prefix[64 * ch + lane] = add_up(ahead, all) - mine;
+        }
+        if (threadIdx.x == 0) p.prefix[bt.batch] = line.total == kTooMany ? 0 : line.total;
+    }
+    if (line.total == 0 || line.total == kTooMany) return;
+    int least = 1;
+    if constexpr (!SHARED) {
+        int longest = line.total / 64;       // (of more than 64 sequences: that many alike)
+        if (line.n_chunks <= 1) {
+            longest = cut.row_tiles(line.lanes) > 0 ? (line.lanes.len_k + kStepTile - 1) / kStepTile : 0;
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off));
+        }
+        least = __builtin_amdgcn_readfirstlane(least_span_mx(line.total, longest, p.a.n_kv_heads, p.unit_rows));
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.prefix[bt.batch + 1] = least;
+    }
+    int at, left, kvh, w = 0;               // place on the line, tiles to work on
+    if constexpr (SHARED) {
+        const WorkOrder order(line.total, 1, p.a.n_kv_heads);
+        const uint32_t block = blockIdx.y * kUnitsRow + blockIdx.x;
+        if ((block >> 3) >= order.count || order.total > (int64_t)gridDim.x * gridDim.y) return;      // (more units than the rows make: as in paged_step_kernel)
+        const int64_t unit = order.unit(block & 7, block >> 3);
+        if (unit < 0) return;
+        kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
+        at = __builtin_amdgcn_readfirstlane((int)unit - kvh * line.total);
+    } else {
+        const StepSpans spans(line.total, p.n_spans, least);
+        const int group_no = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+        w = spans.len < 8 ? wave * (int)gridDim.x + (int)blockIdx.x : group_no * WAVES + wave;
+        const int span = p.kv_heads.div(w);
+        kvh = w - span * p.a.n_kv_heads;
+        at = spans.start(span);
+        left = span < p.n_spans.d ? spans.start(span + 1) - at : 0;
+        if (left <= 0) return;
+    }
+
+    // Row tile `rt` of sequence `seq`; uniform.
+    struct Unit {
+        PagedSeq s;
+        int seq, rt, row0, rows, keys, tiles;
+    };
+    auto unit_of = [&](const PagedSeq& s, int seq, int rt) {
+        Unit u;
+        u.s = s;
+        u.seq = seq;
+        u.rt = rt;
+        u.row0 = rt * R;
+        u.rows = min(R, s.len_q * g - u.row0);
+        u.keys = cut.keys(s, rt);
+        u.tiles = max(SHARED ? 0 : 1, (u.keys + kStepTile - 1) / kStepTile);
+        return u;
+    };
+    auto next_unit = [&](const Unit& u) {
+        PagedSeq s = u.s;
+        int seq = u.seq, rt = u.rt + 1;
+        while (rt >= cut.row_tiles(s)) {
+            rt = 0;
+            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch: what is left has no rows and no keys)
+                seq = 0;
+                s = PagedSeq{0, 0, 0};
+                break;
+            }
+            s = line.seq(seq);
+        }
+        return unit_of(s, seq, rt);
+    };
+    Unit unit;
+    int tile;
+    {
+        const int seq = __builtin_amdgcn_readfirstlane(line.find(at));
+        if (seq < 0) return;
+        at = __builtin_amdgcn_readfirstlane(at);
+        const PagedSeq s = line.seq(seq);
+        const int n_rt = cut.row_tiles(s);
+        int rt = 0;
+        if constexpr (SHARED) {
+            rt = n_rt - 1 - at;              // the longest first
+        } else {
+            for (; rt < n_rt; ++rt) {
+                const int n = cut.tiles(s, rt);
+                if (at < n) break;
+                at -= n;
+            }
+        }
+        if (rt < 0 || rt >= n_rt) return;    // (never, as above)
+        unit = unit_of(s, seq, rt);
+        tile = SHARED ? wave : at;
+        if constexpr (SHARED) left = max(0, (unit.tiles - wave + WAVES - 1) / WAVES);
+    }
+
+    // ---- requests: the tile after the last requested one, in the same unit or a later one.  Page numbers are scalar loads a
+    // tile ahead (they count against another counter than the tiles); an aligned group of eight keys has one page.
+    Unit req = unit;
+    int req_tile = tile, req_left = left;
+    const int kg = m >> 2, vg = c;           // the lane's groups of keys, for K and for V
+    const uint32_t k_lane = (uint32_t)(m & 3) * cache.row_b + 16u * c, v_lane = 4u * m;
+    const uint32_t ks_lane = (uint32_t)c << cache.log_page, vs_lane = (uint32_t)(m >> 2) << cache.log_page;
+    const unsigned char* const k_head = cache.k + (int64_t)kvh * cache.head_b;
+    const unsigned char* const v_head = cache.v + (int64_t)kvh * cache.head_b;
+    const unsigned char* const ks_head = cache.ks + (int64_t)kvh * cache.scale_head_b;
+    const unsigned char* const vs_head = cache.vs + (int64_t)kvh * cache.scale_head_b;
+    uint32_t number[4];
+    auto look_up = [&]() {
+        const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)req.seq * bt.table_len);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            number[i] = req.keys == 0 ? 0 : (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
+    };
+    auto of_group = [](const Off (&x)[4], int i) {
+        const Off lo = i & 1 ? x[1] : x[0], hi = i & 1 ? x[3] : x[2];
+        return i & 2 ? hi : lo;
+    };
+    // Keys past the end come along, from the slots behind the last one or from whatever page is at hand: their scores are masked
+    // and their values become zeros.
+    auto request = [&](MxTile& t) {
+        Off codes[4], scales[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t page = min(number[i], cache.last_page), slot = (uint32_t)(req_tile * kStepTile + 8 * i) & ((1u << cache.log_page) - 1);
+            codes[i] = (Off)page * (Off)cache.page_b + (Off)slot * cache.row_b;
+            scales[i] = (Off)page * (Off)cache.scale_page_b + slot;
+        }
+        const Off ko = of_group(codes, kg) + k_lane, vo = of_group(codes, vg) + v_lane;
+        const Off kso = of_group(scales, kg) + ks_lane, vso = of_group(scales, vg) + vs_lane;
+        t.ks = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(ks_head + kso));
+        t.vs = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vs_head + vso));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            t.k[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k_head + (int64_t)(4 * u) * cache.row_b + ko));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t.v[e] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(v_head + (int64_t)e * cache.row_b + vo));
+        if (--req_left == 0) return;
+        req_tile += STRIDE;
+        if (!SHARED && req_tile == req.tiles) {
+            req = next_unit(req);
+            req_tile = 0;
+        }
+        look_up();
+    };
+
+    // ---- the piece in hand: tiles [piece0, end) of the unit
+    const float sl2 = p.a.scale_log2;
+    int piece0, end, first_vis;
+    int pos[NT], head[NT], last_vis[NT];      // new token, query head and last key of this lane's rows
+    bf16x8 qf[NT][4];
+    f32x4 o[NT][8];
+    float m_run[NT], l_run[NT];
+    auto begin_piece = [&]() {
+        const int last = unit.keys - 1;
+        piece0 = tile;
+        end = SHARED ? unit.tiles : min(unit.tiles, tile + left);
+        first_vis = causal ? unit.s.len_k - unit.s.len_q + cut.group.div(unit.row0) : last;       // last key of the first row
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = unit.row0 + nt * 16 + m;
+            pos[nt] = cut.group.div(r);
+            head[nt] = kvh * g + r - pos[nt] * g;
+            last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + pos[nt]) : last;
+            // rows without a query stay zero and are not stored
+            const __bf16* qrow = p.a.q + (unit.s.q0 + pos[nt]) * p.a.q_stride + (int64_t)head[nt] * kHeadDim + 32 * c;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                u32x4 raw = {0u, 0u, 0u, 0u};
+                if (nt * 16 + m < unit.rows) raw = *reinterpret_cast<const u32x4*>(qrow + 8 * t);
+                qf[nt][t] = __builtin_bit_cast(bf16x8, raw);
+            }
+            m_run[nt] = -INFINITY;
+            l_run[nt] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    auto across = [](float x, auto op) {      // over the four lanes that share a row
+        const uint32_t u = __builtin_bit_cast(uint32_t, x);
+        const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        x = op(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+        const uint32_t v = __builtin_bit_cast(uint32_t, x);
+        const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return op(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+    };
+    // V^T blocks of eight keys a lane, two at a time: block(j, V^T operand)
+    auto blocks_of = [](const uint32_t (&v)[8], const float (&sv)[8], auto block) {
+        auto pair = [&](auto which) {
+            constexpr int P = decltype(which)::value;
+            uint32_t d[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[e], sv[e], P);
+                d[e] = __builtin_bit_cast(uint32_t, x);
+            }
+            u32x4 lo, hi;
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                lo[f] = __builtin_amdgcn_perm(d[2 * f + 1], d[2 * f], 0x05040100u);
+                hi[f] = __builtin_amdgcn_perm(d[2 * f + 1], d[2 * f], 0x07060302u);
+            }
+            block(2 * P, __builtin_bit_cast(bf16x8, lo));
+            block(2 * P + 1, __builtin_bit_cast(bf16x8, hi));
+        };
+        pair(std::integral_constant<int, 0>{});
+        pair(std::integral_constant<int, 1>{});
+        pair(std::integral_constant<int, 2>{});
+        pair(std::integral_constant<int, 3>{});
+    };
+    auto scales_of = [](const u32x2& b, float (&sv)[8]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sv[4 * h] = mx_scale<0>(b[h]);
+            sv[4 * h + 1] = mx_scale<1>(b[h]);
+            sv[4 * h + 2] = mx_scale<2>(b[h]);
+            sv[4 * h + 3] = mx_scale<3>(b[h]);
+        }
+    };
+
+    auto work = [&](MxTile& t) {
+        const int key0 = tile * kStepTile, keys = unit.keys, last = keys - 1;
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float scale = mx_scale_of(t.ks[u] >> (8 * (m & 3)));
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, mx_values(t.k[u][d], scale));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nt][d], s[nt][u], 0, 0, 0);
+            }
+        }
+        // mask, softmax reference (kept lazily: it moves only for a score more than 2^8 ahead of it), weights
+        const bool need_mask = key0 + kStepTile - 1 > min(first_vis, last);
+        bf16x8 pp[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (need_mask) {
+                const int lim = last_vis[nt] - key0 - 8 * c;
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r > lim) s[nt][r >> 2][r & 3] = -INFINITY;
+            }
+            float mx = s[nt][0][0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[nt][r >> 2][r & 3]);
+            mx = across(mx, [](float x, float y) { return fmaxf(x, y); });
+            const float mx2 = mx * sl2;
+            const float m_new = (mx2 > m_run[nt] + 8.f) ? mx2 : m_run[nt];
+            const float m_use = (m_new == -INFINITY) ? 0.f : m_new;   // a row that has seen no key yet
+            const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - m_use);
+            m_run[nt] = m_new;
+            float rs = 0.f;
+            u32x4 packed;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x2 x = {__builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1)], sl2, -m_use)),
+                                 __builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sl2, -m_use))};
+                rs += x[0] + x[1];      // the denominator from the unrounded weights; for the product they are bf16, as everywhere here
+                packed[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+            }
+            pp[nt] = __builtin_bit_cast(bf16x8, packed);
+            l_run[nt] = l_run[nt] * alpha + rs;
+            if (__any(alpha != 1.f)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nt][j][i] *= alpha;
+            }
+        }
+        // values past the end: zero
+        u32x2 vs = t.vs;
+        if (key0 + kStepTile > keys) {
+            const int n = keys - key0 - 8 * c;      // of this lane's
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= n) {
+                    t.v[e] = 0u;
+                    vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
+                }
+        }
+        auto sum_up = [&](int j, const bf16x8& vf) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nt], o[nt][j], 0, 0, 0);
+        };
+        // A value that some of the rows do not see reaches them as 0 x value, which NaN (and what exceeds bf16) is not.  In tiles
+        // with such keys their values are zeroed for the product, and each is added by itself to the rows that see it.
+        uint32_t odd_keys = 0;
+        if (min(key0 + kStepTile - 1, last) > first_vis) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((vs[e >> 2] >> 8 * (e & 3) & 0xffu) >= 253u && key0 + 8 * c + e > first_vis) odd |= 1u << e;
+            if (__any(odd != 0)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint64_t b = __ballot(odd >> e & 1);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (b >> 16 * i & 0xffff) odd_keys |= 1u << (8 * i + e);
+                }
+                odd_keys = __builtin_amdgcn_readfirstlane(odd_keys);
+                const uint32_t sv_bytes[2] = {vs[0], vs[1]};
+                for (uint32_t rest = odd_keys; rest != 0; rest &= rest - 1) {
+                    const int key = __builtin_ctz(rest);
+                    uint32_t v1[8];
+                    float s1[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool it = 8 * c + e == key;
+                        v1[e] = it ? t.v[e] : 0u;
+                        s1[e] = it ? mx_scale_of(sv_bytes[e >> 2] >> 8 * (e & 3) & 0xffu) : 1.f;
+                    }
+                    blocks_of(v1, s1, [&](int j, const bf16x8& vf) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[nt][j][i] += key0 + key <= last_vis[nt] ? x[i] : 0.f;
+                        }
+                    });
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (odd_keys >> (8 * c + e) & 1) {
+                        t.v[e] = 0u;
+                        vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
+                    }
+            }
+        }
+        float sv[8];
+        scales_of(vs, sv);
+        blocks_of(t.v, sv, sum_up);
+    };
+
+    // ---- the unit's result, or the piece's into its slot
+    auto finish_piece = [&]() {
+        const bool whole = piece0 == 0 && end == unit.tiles;
+        const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float l_tot = across(l_run[nt], [](float x, float y) { return x + y; });
+            if (nt * 16 + m < unit.rows) {
+                const int token = unit.s.q0 + pos[nt];
+                const bool none = l_tot == 0.f || unit.keys == 0;       // (without keys the values may be anything, and the sums NaN)
+                const float inv = none ? 0.f : 1.f / l_tot;
+                const float lse = none ? -INFINITY : (m_run[nt] + __builtin_amdgcn_logf(l_tot)) * kLn2;     // NaN from NaN weights
+                if (c == 0) {
+                    if (whole) p.a.lse[(int64_t)head[nt] * bt.total_q + token] = lse;
+                    else p.part_lse[slot_row + nt * 16 + m] = lse;
+                }
+                const int64_t row = whole ? (int64_t)token * p.a.n_q_heads + head[nt] : slot_row + nt * 16 + m;
+                float* const dst = whole ? static_cast<float*>(p.a.out) : p.part_out;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x8 x;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = none ? 0.f : o[nt][j][i] * inv;
+                    const int64_t idx = row * kHeadDim + 32 * c + 8 * i;
+                    if (!whole || p.a.out_f32) *reinterpret_cast<f32x8*>(dst + idx) = x;
+                    else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(x, bf16x8);
+                }
+            }
+        }
+    };
+
+    MxTile ring[S];
+    if (req_left > 0) look_up();
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+        if (req_left > 0) request(ring[i]);
+    begin_piece();
+    if constexpr (SHARED) {
+        auto step = [&](MxTile& t) {
+            work(t);
+            tile += STRIDE;
+            if (req_left > 0) request(t);
+            return --left > 0;
+        };
+        if (left > 0)
+            while (step(ring[0]) && step(ring[1])) {}
+        // ---- the wavefronts' results of every row are joined, 16 rows at a time.  O goes to LDS in 16-byte chunks of 4 dims,
+        // chunk ch of row r at slot ch * 16 + (r ^ ch % 16): writers (a row per lane) and readers (a chunk per lane, so that a row leaves
+        // as one run) touch all banks evenly.
+        float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            __syncthreads();
+            const float l_tot = across(l_run[nt], [](float x, float y) { return x + y; });
+            if (c == 0) {
+                join_m[wave * 16 + m] = m_run[nt];
+                join_l[wave * 16 + m] = l_tot;
+            }
+            f32x4* const po = reinterpret_cast<f32x4*>(joint_o) + wave * 512;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int ch = 8 * c + 2 * i + h;
+                    po[ch * 16 + (m ^ (ch & 15))] = f32x4{o[nt][4 * h][i], o[nt][4 * h + 1][i], o[nt][4 * h + 2][i], o[nt][4 * h + 3][i]};
+                }
+            __syncthreads();
+            if (threadIdx.x < WAVES * 16) {   // one thread per (row, wavefront): the wavefront's weight
+                const int r = threadIdx.x & 15, k = threadIdx.x >> 4;
+                float mx = -INFINITY, den = 0.f;
+#pragma unroll
+                for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, join_m[i * 16 + r]);
+                const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+                for (int i = 0; i < WAVES; ++i) den += join_l[i * 16 + r] * __builtin_amdgcn_exp2f(join_m[i * 16 + r] - ref);
+                const float inv = den == 0.f ? 0.f : 1.f / den;
+                join_w[k * 16 + r] = __builtin_amdgcn_exp2f(join_m[k * 16 + r] - ref) * inv;
+                const int flat = unit.row0 + nt * 16 + r, at_pos = cut.group.div(flat);
+                if (k == 0 && nt * 16 + r < unit.rows)
+                    p.a.lse[(int64_t)(kvh * g + flat - at_pos * g) * bt.total_q + unit.s.q0 + at_pos] =
+                        den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
+            }
+            __syncthreads();
+            const int ch = threadIdx.x & 31;
+#pragma unroll
+            for (int pass = 0; pass < 8 / WAVES; ++pass) {
+                const int r = pass * 2 * WAVES + (threadIdx.x >> 5), flat = unit.row0 + nt * 16 + r, at_pos = cut.group.div(flat);
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < WAVES; ++k) {
+                    const float wgt = join_w[k * 16 + r];
+                    const f32x4 y = reinterpret_cast<const f32x4*>(joint_o)[k * 512 + ch * 16 + (r ^ (ch & 15))];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = fmaf(wgt, y[i], x[i]);
+                }
+                if (nt * 16 + r < unit.rows) {
+                    const int64_t idx = ((int64_t)(unit.s.q0 + at_pos) * p.a.n_q_heads + kvh * g + flat - at_pos * g) * kHeadDim + 4 * ch;
+                    if (p.a.out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.a.out) + idx) = x;
+                    else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(x, bf16x4);
+                }
+            }
+        }
+    } else {
+        auto step = [&](MxTile& t) {      // false: the span has ended
+            work(t);
+            --left;
+            ++tile;
+            if (req_left > 0) request(t);
+            if (tile < end) return true;
+            finish_piece();
+            if (left <= 0) return false;
+            unit = next_unit(unit);
+            tile = 0;
+            begin_piece();
+            return true;
+        };
+        static_assert(S >= 2 && S <= 4, "stages are written out");
+        for (;;) {
+            if (!step(ring[0])) return;
+            if (!step(ring[1])) return;
+            if constexpr (S > 2)
+                if (!step(ring[2])) return;
+            if constexpr (S > 3)
+                if (!step(ring[3])) return;
+        }
+    }
+}
+
+}  // namespace pec

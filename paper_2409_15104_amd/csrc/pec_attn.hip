@@ -27,6 +27,7 @@
 #include "paged_mx_common.hpp"
 #include "paged_mx_read_kernel.hpp"
 #include "paged_mx_simple_kernel.hpp"
+#include "paged_mx_step_kernel.hpp"
 #include "paged_simple_kernel.hpp"
 #include "paged_step_kernel.hpp"
 #include "probes.hpp"
