@@ -162,6 +162,64 @@ void launch_paged_merge(const PagedStepParams& s, int cu, int tokens, int64_t le
         hipLaunchKernelGGL(paged_merge_kernel<16>, dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
 }
 
+// The work list of sequences with more than few_rows rows per KV head, the pipelined kernel on it, and the merge of its ranges.
+int launch_paged_list(const PagedAttnParams& p, const PagedLayout& l, int cu, int few_rows, char* ws, hipStream_t st) {
+    if (l.capacity * l.units > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
+    PagedListParams w{};
+    w.batch = p.batch;
+    w.bm = l.bm;
+    w.log_bm = 8 - l.log_heads;
+    w.group = p.group;
+    w.units = l.units;
+    w.causal = p.causal;
+    w.few_rows = few_rows;
+    w.capacity = (int32_t)l.capacity;
+    w.slot_capacity = (int32_t)l.slots;
+    w.cu = cu;
+    w.work = reinterpret_cast<WorkItem*>(ws + l.off_work);
+    w.counters = reinterpret_cast<int32_t*>(ws + l.off_counters);
+    w.splits = reinterpret_cast<PagedSplit*>(ws + l.off_splits);
+    hipLaunchKernelGGL(paged_list_kernel, dim3(1), dim3(1024), 0, st, w);
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    FwdParams f{};
+    f.q = p.q;
+    f.k = reinterpret_cast<const __bf16*>(p.cache.k);
+    f.v = reinterpret_cast<const __bf16*>(p.cache.v);
+    f.out = p.out;
+    f.lse = p.lse;
+    f.lse_stride = p.batch.total_q;
+    f.causal = p.causal;
+    f.n_q_heads = p.n_q_heads;
+    f.n_kv_heads = p.n_kv_heads;
+    f.group = p.group;
+    f.log_heads = l.log_heads;
+    f.n_items = (int32_t)l.capacity;
+    f.out_f32 = p.out_f32;
+    f.scale_log2 = p.scale_log2;
+    f.work = w.work;
+    f.n_work = w.counters;
+    f.sched = w.counters + 8;
+    f.q_row_stride = p.q_stride;
+    f.part_out = reinterpret_cast<float*>(ws);
+    f.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+    f.table = p.batch.table_len > 0 ? p.batch.table : p.batch.cu_q;      // (a word to look at where there is no page: no key is in it)
+    f.table_len = p.batch.table_len;
+    f.page_b = p.cache.page_b;
+    f.row_b = p.cache.row_b;
+    f.head_b = p.cache.head_b;
+    f.last_page = p.cache.last_page;
+    f.log_page = p.cache.log_page;
+    const int64_t groups = std::min<int64_t>(cu, (l.capacity * l.units + 7) / 8 * 8);
+    hipLaunchKernelGGL(fwd_il_kernel<kFwdPaged>, dim3((unsigned)groups), dim3(512), 0, st, f);
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    if (l.slots > 1) {
+        hipLaunchKernelGGL(paged_ranges_merge_kernel, dim3((unsigned)std::min<int64_t>(l.slots / 2 * l.units * 32, 4 * cu)), dim3(256), 0, st, w,
+                           f.part_out, f.part_lse, l.log_heads, p.n_q_heads, p.out_f32, p.out, p.lse);
+        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    }
+    return PEC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -291,60 +349,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     }
     if (!cut.list) return PEC_OK;
-    if (l.capacity * l.units > 0x7fffffff) return PEC_ERR_UNSUPPORTED;
-    PagedListParams w{};
-    w.batch = p.batch;
-    w.bm = l.bm;
-    w.log_bm = 8 - l.log_heads;
-    w.group = g;
-    w.units = l.units;
-    w.causal = p.causal;
-    w.few_rows = cut.steps ? cut.few_rows : 0;
-    w.capacity = (int32_t)l.capacity;
-    w.slot_capacity = (int32_t)l.slots;
-    w.cu = cu;
-    w.work = reinterpret_cast<WorkItem*>(ws + l.off_work);
-    w.counters = reinterpret_cast<int32_t*>(ws + l.off_counters);
-    w.splits = reinterpret_cast<PagedSplit*>(ws + l.off_splits);
-    hipLaunchKernelGGL(paged_list_kernel, dim3(1), dim3(1024), 0, st, w);
-    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-    FwdParams f{};
-    f.q = p.q;
-    f.k = reinterpret_cast<const __bf16*>(p.cache.k);
-    f.v = reinterpret_cast<const __bf16*>(p.cache.v);
-    f.out = out;
-    f.lse = lse;
-    f.lse_stride = batch->total_q;
-    f.causal = p.causal;
-    f.n_q_heads = p.n_q_heads;
-    f.n_kv_heads = p.n_kv_heads;
-    f.group = g;
-    f.log_heads = l.log_heads;
-    f.n_items = (int32_t)l.capacity;
-    f.out_f32 = p.out_f32;
-    f.scale_log2 = p.scale_log2;
-    f.work = w.work;
-    f.n_work = w.counters;
-    f.sched = w.counters + 8;
-    f.q_row_stride = p.q_stride;
-    f.part_out = reinterpret_cast<float*>(ws);
-    f.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
-    f.table = p.batch.table_len > 0 ? p.batch.table : p.batch.cu_q;      // (a word to look at where there is no page: no key is in it)
-    f.table_len = p.batch.table_len;
-    f.page_b = p.cache.page_b;
-    f.row_b = p.cache.row_b;
-    f.head_b = p.cache.head_b;
-    f.last_page = p.cache.last_page;
-    f.log_page = p.cache.log_page;
-    const int64_t groups = std::min<int64_t>(cu, (l.capacity * l.units + 7) / 8 * 8);
-    hipLaunchKernelGGL(fwd_il_kernel<kFwdPaged>, dim3((unsigned)groups), dim3(512), 0, st, f);
-    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-    if (l.slots > 1) {
-        hipLaunchKernelGGL(paged_ranges_merge_kernel, dim3((unsigned)std::min<int64_t>(l.slots / 2 * l.units * 32, 4 * cu)), dim3(256), 0, st, w,
-                           f.part_out, f.part_lse, l.log_heads, p.n_q_heads, p.out_f32, out, lse);
-        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-    }
-    return PEC_OK;
+    return launch_paged_list(p, l, cu, cut.steps ? cut.few_rows : 0, ws, st);
 }
 
 }  // extern "C"

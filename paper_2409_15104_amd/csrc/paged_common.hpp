@@ -41,6 +41,10 @@ struct PagedBatch {
     const int32_t* table;        // [batch][table_len]
     int32_t batch, table_len, total_q;
     int32_t max_keys;            // table_len pages, at most 2^30 keys
+    // of a cache in 4 bits, or null: where a sequence's keys are in bf16 as well, first page, or -1; the launch is for those
+    // sequences (area_side 1) or for the others (0), which to the other launch are without queries
+    const int32_t* area;
+    int32_t area_side;
 };
 
 struct PagedSeq {
@@ -51,6 +55,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& b, int i) {
     s.q0 = min(max(b.cu_q[i], 0), b.total_q);
     s.len_q = min(max(b.cu_q[i + 1], s.q0), b.total_q) - s.q0;
     s.len_k = min(max(b.len_k[i], 0), b.max_keys);
+    if (b.area && (b.area[i] >= 0 ? 1 : 0) != b.area_side) s.len_q = 0;
     return s;
 }
 

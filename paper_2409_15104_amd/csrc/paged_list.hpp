@@ -148,6 +148,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
     // ---- items of sequence `b`, from place `pos0` of the list on: range by range, the last tile first
     auto place = [&](int b, const PagedSeq& sq, int pos0) {
         const PagedTiles t(sq, p);
+        const int table_row = bt.area ? bt.area[b] : b;
         for (int tile = lane; tile < t.n; tile += 64) {
             const int keys = t.keys(tile), n_ranges = max(1, (int)(((int64_t)keys + range - 1) / range));
             int slot0 = -1;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
                 if (r > 0) pos += t.n - (r == 1 ? 0 : t.first_beyond((r - 1) * range));
                 const int key0 = r * range;
                 if ((uint32_t)pos < (uint32_t)p.capacity)
-                    p.work[pos] = WorkItem{sq.q0, sq.len_q, b, sq.len_k, tile, slot0 < 0 ? -1 : slot0 + r,
+                    p.work[pos] = WorkItem{sq.q0, sq.len_q, table_row, sq.len_k, tile, slot0 < 0 ? -1 : slot0 + r,
                                            {n_ranges > 1 ? key0 : 0, n_ranges > 1 ? min(keys, key0 + range) : keys}};
             }
         }

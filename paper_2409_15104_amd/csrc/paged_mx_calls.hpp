@@ -36,9 +36,74 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
     return PEC_OK;
 }
 
+// Workspace of pec_attn_paged_mx: pec_attn_paged's, then the area (paged_mx_area_kernel.hpp) of so many pages.
+struct MxLayout {
+    PagedLayout paged;
+    size_t off_area, off_used, off_owner, off_table, off_k, off_v, bytes;
+};
+MxLayout mx_layout(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t pages) {
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    MxLayout l;
+    l.paged = paged_layout(compute_units(), shape, batch, total_q);
+    l.off_area = up(l.paged.bytes);
+    l.off_used = up(l.off_area + (size_t)batch * sizeof(int32_t));
+    l.off_owner = l.off_used + 256;
+    l.off_table = l.off_owner + (size_t)pages * sizeof(int32_t);
+    l.off_k = up(l.off_table + (size_t)(pages + 1) * sizeof(int32_t));
+    l.off_v = l.off_k + (size_t)pages * shape->n_kv_heads * kMxAreaHeadBytes;
+    l.bytes = l.off_v + (size_t)pages * shape->n_kv_heads * kMxAreaHeadBytes;
+    return l;
+}
+// Pages that a workspace of so many bytes, at least those of no page, has room for.
+int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, size_t bytes) {
+    const size_t none = mx_layout(shape, batch, total_q, 0).bytes, page = 2 * (size_t)shape->n_kv_heads * kMxAreaHeadBytes + 2 * sizeof(int32_t);
+    int64_t pages = (int64_t)std::min<size_t>((bytes - none + 256) / page, 0x7fffffff);
+    while (pages > 0 && mx_layout(shape, batch, total_q, pages).bytes > bytes) --pages;      // (what is rounded up: once or not at all)
+    return pages;
+}
+
 // Of row tiles of 16 that a wavefront of paged_mx_step_kernel takes, for sequences of up to so many rows; wavefronts per workgroup.
 int mx_step_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 constexpr int mx_step_waves(int nt) { return nt == 4 ? 4 : 8; }
+
+// The sequences of the call (of its side of the area) straight from their codes: spans and their merge.
+int mx_steps(const PagedAttnParams& p, const PagedMx& mx, int page_size, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
+             hipStream_t st) {
+    const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
+    const int g = p.group, nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
+    // offsets of the last page's last element, from a head's first one
+    const int64_t furthest = (int64_t)mx.last_page * mx.page_b + (int64_t)page_size * mx.row_b,
+                  furthest_scale = (int64_t)mx.last_page * mx.scale_page_b + (int64_t)page_size * kMxGroups;
+    const bool wide = std::max(furthest, furthest_scale) > 0xffffffffll;
+    PagedStepParams s{};
+    s.a = p;
+    s.part_out = reinterpret_cast<float*>(ws);
+    s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
+    s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
+    s.cut = StepCut{fast_div(g), nt == 1 ? 4 : nt == 2 ? 5 : 6, p.causal, 0x7fffffff};
+    const int waves = cu * waves_per;
+    if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
+    s.n_spans = fast_div(waves / p.n_kv_heads);
+    s.kv_heads = fast_div(p.n_kv_heads);
+    s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
+    const int64_t row_tiles = total_q * g / (16 * nt) + batch;
+    if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
+    const dim3 grid((unsigned)cu), threads((unsigned)waves_per * 64);
+    auto launch = [&](auto tiles, auto is_wide) {
+        constexpr int NT = decltype(tiles)::value;
+        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), 2, false, decltype(is_wide)::value>), grid, threads, 0, st, s, mx);
+    };
+    auto launch_nt = [&](auto is_wide) {
+        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_wide);
+        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_wide);
+        else launch(std::integral_constant<int, 4>{}, is_wide);
+    };
+    if (wide) launch_nt(std::true_type{});
+    else launch_nt(std::false_type{});
+    if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+    launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
+    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+}
 
 }  // namespace
 
@@ -88,8 +153,10 @@ int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
 }
 
 size_t pec_paged_mx_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t total_k) {
-    if (total_k < 0) return 0;
-    return pec_paged_workspace_bytes(shape, batch, total_q);
+    if (!shape || shape->n_q_heads <= 0 || shape->n_kv_heads <= 0 || batch < 0 || total_q < 0 || total_k < 0) return 0;
+    if (shape->n_q_heads % shape->n_kv_heads != 0) return 0;
+    const int64_t pages = total_k > 0 ? std::min<int64_t>(total_k / kMxAreaPage + batch, 0x7fffffff) : 0;      // (a sequence's last page is in part its own)
+    return mx_layout(shape, batch, total_q, pages).bytes;
 }
 
 int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, const void* q,
@@ -131,39 +198,51 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
-    // offsets of the last page's last element, from a head's first one
-    const int64_t furthest = (int64_t)mx.last_page * mx.page_b + (int64_t)cache->page_size * mx.row_b,
-                  furthest_scale = (int64_t)mx.last_page * mx.scale_page_b + (int64_t)cache->page_size * kMxGroups;
-    const bool wide = std::max(furthest, furthest_scale) > 0xffffffffll;
-    PagedStepParams s{};
-    s.a = p;
-    const int nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
-    s.part_out = reinterpret_cast<float*>(ws);
-    s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
-    s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-    s.cut = StepCut{fast_div(g), nt == 1 ? 4 : nt == 2 ? 5 : 6, p.causal, 0x7fffffff};
-    const int waves = cu * waves_per;
-    if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
-    s.n_spans = fast_div(waves / p.n_kv_heads);
-    s.kv_heads = fast_div(p.n_kv_heads);
-    s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
-    const int64_t row_tiles = batch->total_q * g / (16 * nt) + batch->batch;
-    if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
-    const dim3 grid((unsigned)cu), threads((unsigned)waves_per * 64);
-    auto launch = [&](auto tiles, auto is_wide) {
-        constexpr int NT = decltype(tiles)::value;
-        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), 2, false, decltype(is_wide)::value>), grid, threads, 0, st, s, mx);
-    };
-    auto launch_nt = [&](auto is_wide) {
-        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_wide);
-        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_wide);
-        else launch(std::integral_constant<int, 4>{}, is_wide);
-    };
-    if (wide) launch_nt(std::true_type{});
-    else launch_nt(std::false_type{});
+    // sequences with many rows: in the area, if it is there.  `both`: few-row sequences beside them, which stay with their codes;
+    // else all are taken there, and what finds no room, if that can be, is left to the steps as well.
+    const int64_t pages = l.capacity > 0 && len_q * g > kPagedFewRows ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
+    const bool list = pages > 0;
+    const bool both = batch->batch - (batch->total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2;
+    const bool room = batch->batch * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
+    MxAreaParams a{};
+    if (list) {
+        const MxLayout m = mx_layout(shape, batch->batch, batch->total_q, pages);
+        a.cache = mx;
+        a.batch = p.batch;
+        a.group = g;
+        a.few_rows = both ? kPagedFewRows : 0;
+        a.capacity = (int32_t)pages;
+        a.n_kv_heads = p.n_kv_heads;
+        a.area = reinterpret_cast<int32_t*>(ws + m.off_area);
+        a.owner = reinterpret_cast<int32_t*>(ws + m.off_owner);
+        a.table = reinterpret_cast<int32_t*>(ws + m.off_table);
+        a.used = reinterpret_cast<int32_t*>(ws + m.off_used);
+        a.k = reinterpret_cast<unsigned char*>(ws + m.off_k);
+        a.v = reinterpret_cast<unsigned char*>(ws + m.off_v);
+        hipLaunchKernelGGL(paged_mx_area_kernel, dim3(1), dim3(1024), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
+        p.batch.area = a.area;
+    }
+    if (!list || both || !room) {
+        p.batch.area_side = 0;
+        if (int rc = mx_steps(p, mx, cache->page_size, l, cu, list && both ? std::min<int64_t>(len_q, kPagedFewRows) : len_q, len_k, ws, st)) return rc;
+    }
+    if (!list) return PEC_OK;
+    const int64_t fill = std::min<int64_t>(pages * p.n_kv_heads, (int64_t)cu * 16);
+    hipLaunchKernelGGL(paged_mx_fill_kernel, dim3((unsigned)fill), dim3(256), 0, st, a);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
-    launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
-    return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    p.batch.area_side = 1;
+    p.batch.table = a.table;
+    p.batch.table_len = 1;
+    p.cache.k = a.k;
+    p.cache.v = a.v;
+    p.cache.page_b = (int64_t)p.n_kv_heads * kMxAreaHeadBytes;
+    p.cache.row_b = kRowBytes;
+    p.cache.head_b = kMxAreaHeadBytes;
+    p.cache.last_page = (uint32_t)(pages - 1);
+    p.cache.log_page = 6;
+    static_assert(kMxAreaPage == 64, "log_page");
+    return launch_paged_list(p, l, cu, 0, ws, st);
 }
 
 }  // extern "C"

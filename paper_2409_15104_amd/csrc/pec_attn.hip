@@ -24,6 +24,7 @@
 #include "kernel_choice.hpp"
 #include "norm_rope_kernel.hpp"
 #include "paged_list.hpp"
+#include "paged_mx_area_kernel.hpp"
 #include "paged_mx_common.hpp"
 #include "paged_mx_read_kernel.hpp"
 #include "paged_mx_simple_kernel.hpp"

@@ -159,3 +159,32 @@ def test_attention(seqs, hq, hkv, page, by_head, causal, flags):
         pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, causal=causal, out_dtype=dtype, flags=flags, out=out, lse=lse)
         assert_attention(out, lse, ref, "%s %s" % (seqs, dtype), plain=flags != 0)
         assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
+
+
+@pytest.mark.parametrize("room", [0, 100, 200, 100000])
+@pytest.mark.parametrize("hints", [True, False])
+@pytest.mark.parametrize("hq,hkv,page", [(8, 2, 16), (16, 16, 8), (6, 1, 128)])
+def test_attention_with_room_for_some_sequences(hq, hkv, page, hints, room):
+    """Keys of sequences with many rows in bf16, as far as the workspace goes; all of them give the same."""
+    seqs = [(1, 190), (70, 70), (150, 400), (1, 5), (0, 90), (40, 64), (1, 1), (300, 301), (1, 700)]
+    b = MxBatch(13, hq, hkv, page, seqs, spare_rows=2)
+    cache, table, cu, len_k = caches(b)
+    ref = attention(b)
+    ws = torch.full((pec.pec_paged_mx_workspace_bytes(hq, hkv, len(seqs), b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
+    out = torch.full((b.total, hq, 128), 55.0, dtype=torch.float32, device=DEV)
+    lse = torch.full((hq, b.total), 55.0, device=DEV)
+    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=300 if hints else 0, max_len_k=700 if hints else 0,
+                          out_dtype=torch.float32, out=out, lse=lse, workspace=ws)
+    assert_attention(out, lse, ref)
+    assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
+
+
+@pytest.mark.parametrize("room", [0, 1500, 100000])
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_chunk(causal, room):
+    b = MxBatch(14, 8, 2, 32, [(333, 1500)])
+    cache, table, cu, len_k = caches(b)
+    table = table[:, :47].contiguous()      # no wider than the sequence: then all of it has room for certain
+    ws = torch.full((pec.pec_paged_mx_workspace_bytes(8, 2, 1, b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
+    out, lse = pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, causal=causal, workspace=ws)
+    assert_attention(out, lse, attention(b, causal))
