@@ -63,18 +63,20 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
 }
 
 // Of row tiles of 16 that a wavefront of paged_mx_step_kernel takes, for sequences of up to so many rows; wavefronts per workgroup.
+#ifndef MX_S
+#define MX_S(nt) 2
+#endif
 int mx_step_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-constexpr int mx_step_waves(int nt) { return nt == 4 ? 4 : 8; }
+#ifndef MX_W
+#define MX_W(nt) (nt == 4 ? 4 : 8)
+#endif
+constexpr int mx_step_waves(int nt) { return MX_W(nt); }
 
 // The sequences of the call (of its side of the area) straight from their codes: spans and their merge.
-int mx_steps(const PagedAttnParams& p, const PagedMx& mx, int page_size, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
+int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
              hipStream_t st) {
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
     const int g = p.group, nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
-    // offsets of the last page's last element, from a head's first one
-    const int64_t furthest = (int64_t)mx.last_page * mx.page_b + (int64_t)page_size * mx.row_b,
-                  furthest_scale = (int64_t)mx.last_page * mx.scale_page_b + (int64_t)page_size * kMxGroups;
-    const bool wide = std::max(furthest, furthest_scale) > 0xffffffffll;
     PagedStepParams s{};
     s.a = p;
     s.part_out = reinterpret_cast<float*>(ws);
@@ -89,16 +91,16 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, int page_size, const P
     const int64_t row_tiles = total_q * g / (16 * nt) + batch;
     if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
     const dim3 grid((unsigned)cu), threads((unsigned)waves_per * 64);
-    auto launch = [&](auto tiles, auto is_wide) {
+    auto launch = [&](auto tiles, auto is_small) {
         constexpr int NT = decltype(tiles)::value;
-        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), 2, false, decltype(is_wide)::value>), grid, threads, 0, st, s, mx);
+        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), MX_S(NT), false, decltype(is_small)::value>), grid, threads, 0, st, s, mx);
     };
-    auto launch_nt = [&](auto is_wide) {
-        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_wide);
-        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_wide);
-        else launch(std::integral_constant<int, 4>{}, is_wide);
+    auto launch_nt = [&](auto is_small) {
+        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_small);
+        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_small);
+        else launch(std::integral_constant<int, 4>{}, is_small);
     };
-    if (wide) launch_nt(std::true_type{});
+    if (mx.log_page < 4) launch_nt(std::true_type{});
     else launch_nt(std::false_type{});
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
@@ -204,13 +206,14 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const bool list = pages > 0;
     const bool both = batch->batch - (batch->total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2;
     const bool room = batch->batch * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
+    const int few = g <= 16 ? 16 : g <= 32 ? 32 : 64;      // rows of such a sequence at most
     MxAreaParams a{};
     if (list) {
         const MxLayout m = mx_layout(shape, batch->batch, batch->total_q, pages);
         a.cache = mx;
         a.batch = p.batch;
         a.group = g;
-        a.few_rows = both ? kPagedFewRows : 0;
+        a.few_rows = both ? few : 0;
         a.capacity = (int32_t)pages;
         a.n_kv_heads = p.n_kv_heads;
         a.area = reinterpret_cast<int32_t*>(ws + m.off_area);
@@ -225,7 +228,7 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     }
     if (!list || both || !room) {
         p.batch.area_side = 0;
-        if (int rc = mx_steps(p, mx, cache->page_size, l, cu, list && both ? std::min<int64_t>(len_q, kPagedFewRows) : len_q, len_k, ws, st)) return rc;
+        if (int rc = mx_steps(p, mx, l, cu, list && both ? std::max<int64_t>(1, std::min<int64_t>(len_q, few / g)) : len_q, len_k, ws, st)) return rc;
     }
     if (!list) return PEC_OK;
     const int64_t fill = std::min<int64_t>(pages * p.n_kv_heads, (int64_t)cu * 16);

@@ -8,10 +8,12 @@
 //
 // Products are 16 x 16 x 32 (lane l: m = l % 16, c = l / 16; A rows m, B columns m, k-slots 8 c ... 8 c + 7; C column m, rows 4 c + i).
 // Scores, S^T = K Q^T: the contraction runs over dims in any order that K and Q agree on, so lane (m, c) takes dims 32 c ... 32 c + 31
-// of a key, 16 bytes of codes in one load and exactly one scale group, eight dims for each of four products.  Row 4 c + i of product u is
-// key 8 c + 4 u + i, so that lane c ends up with the scores of the eight keys 8 c ... 8 c + 7, which is the order in which
-// O^T += V^T P^T wants them.  There row m of block j is dim 8 m + j: a lane needs of each of its eight keys the four bytes of dims
+// of key m, 16 bytes of codes in one load and exactly one scale group, eight dims for each of four products.  Of the tile's two
+// halves of 16 keys lane c ends up with the scores of keys 4 c + i and 16 + 4 c + i, which are its eight k-slots of
+// O^T += V^T P^T.  There row m of block j is dim 8 m + j: a lane needs of each of its eight keys the four bytes of dims
 // 8 m ... 8 m + 7, converts them in pairs of dims and exchanges halves between neighbouring keys, two instructions for two values.
+// Every load instruction stays inside 16 keys, so with pages of 16 keys and more its page is a scalar base and nothing about it is
+// worked out per lane; pages of eight take a path of their own (SMALL).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,6 +23,12 @@
 #include "paged_mx_common.hpp"
 #include "paged_step_kernel.hpp"
 
+#ifndef MX_LS
+#define MX_LS(x) __builtin_nontemporal_load(x)
+#endif
+#ifndef MX_LC
+#define MX_LC(x) __builtin_nontemporal_load(x)
+#endif
 namespace pec {
 
 // Steps that a span should have at least, as least_span(), a step taking its wavefront 0.6 us.
@@ -30,17 +38,16 @@ __device__ __forceinline__ int least_span_mx(int total, int longest, int n_kv_he
 }
 
 struct MxTile {              // 32 keys, as lane (m, c) takes them
-    u32x4 k[2];              // dims 32 c ... 32 c + 31 of keys 8 (m / 4) + 4 u + m % 4
-    uint32_t v[8];           // dims 8 m ... 8 m + 7 of keys 8 c + e
-    u32x2 ks, vs;            // scale bytes of keys 8 (m / 4) ... + 7 for group c, of keys 8 c ... + 7 for group m / 4
+    u32x4 k[2];              // dims 32 c ... 32 c + 31 of key 16 u + m
+    uint32_t v[8];           // dims 8 m ... 8 m + 7 of keys 16 u + 4 c + i at [4 u + i]
+    uint32_t ks[2], vs[2];   // the scale byte of key 16 u + m for group c, those of keys 16 u + 4 c ... + 3 for group m / 4
 };
 
-// WIDE: offsets in the cache need more than 32 bits.
-template <int NT, int WAVES, int S, bool SHARED, bool WIDE>
+// SMALL: pages of eight keys.
+template <int NT, int WAVES, int S, bool SHARED, bool SMALL>
 __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const PagedStepParams p, const PagedMx cache) {
     constexpr int R = 16 * NT;
     constexpr int STRIDE = SHARED ? WAVES : 1;
-    using Off = std::conditional_t<WIDE, uint64_t, uint32_t>;
     __shared__ __attribute__((aligned(1024))) float joint_o[SHARED ? WAVES * 16 * kHeadDim : 1];
     __shared__ float joint[SHARED ? 3 * WAVES * 16 : 1];
     __shared__ int32_t chunk_sum[kPagedChunks];
@@ -147,46 +154,56 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     }
 
     // ---- requests: the tile after the last requested one, in the same unit or a later one.  Page numbers are scalar loads a
-    // tile ahead (they count against another counter than the tiles); an aligned group of eight keys has one page.
+    // tile ahead (they count against another counter than the tiles).
     Unit req = unit;
     int req_tile = tile, req_left = left;
-    const int kg = m >> 2, vg = c;           // the lane's groups of keys, for K and for V
-    const uint32_t k_lane = (uint32_t)(m & 3) * cache.row_b + 16u * c, v_lane = 4u * m;
-    const uint32_t ks_lane = (uint32_t)c << cache.log_page, vs_lane = (uint32_t)(m >> 2) << cache.log_page;
     const unsigned char* const k_head = cache.k + (int64_t)kvh * cache.head_b;
     const unsigned char* const v_head = cache.v + (int64_t)kvh * cache.head_b;
     const unsigned char* const ks_head = cache.ks + (int64_t)kvh * cache.scale_head_b;
     const unsigned char* const vs_head = cache.vs + (int64_t)kvh * cache.scale_head_b;
-    uint32_t number[4];
+    const uint32_t slot_mask = (1u << cache.log_page) - 1;
+    // lane offsets from the first key of a half (of the page that the lane's key is in)
+    const uint32_t k_lane = (uint32_t)(SMALL ? m & 7 : m) * cache.row_b + 16u * c;
+    const uint32_t ks_lane = ((uint32_t)c << cache.log_page) + (SMALL ? m & 7 : m);
+    const uint32_t vs_lane = ((uint32_t)(m >> 2) << cache.log_page) + 4u * (SMALL ? c & 1 : c);
+    uint32_t v_lane[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v_lane[i] = (4u * (SMALL ? c & 1 : c) + i) * cache.row_b + 4u * m;
+    uint32_t number[SMALL ? 4 : 2];
     auto look_up = [&]() {
         const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)req.seq * bt.table_len);
+        constexpr int KEYS = SMALL ? 8 : 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            number[i] = req.keys == 0 ? 0 : (uint32_t)table[min(req_tile * kStepTile + 8 * i, req.keys - 1) >> cache.log_page];
-    };
-    auto of_group = [](const Off (&x)[4], int i) {
-        const Off lo = i & 1 ? x[1] : x[0], hi = i & 1 ? x[3] : x[2];
-        return i & 2 ? hi : lo;
+        for (int i = 0; i < kStepTile / KEYS; ++i)
+            number[i] = req.keys == 0 ? 0 : min((uint32_t)table[min(req_tile * kStepTile + KEYS * i, req.keys - 1) >> cache.log_page], cache.last_page);
     };
     // Keys past the end come along, from the slots behind the last one or from whatever page is at hand: their scores are masked
     // and their values become zeros.
     auto request = [&](MxTile& t) {
-        Off codes[4], scales[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t page = min(number[i], cache.last_page), slot = (uint32_t)(req_tile * kStepTile + 8 * i) & ((1u << cache.log_page) - 1);
-            codes[i] = (Off)page * (Off)cache.page_b + (Off)slot * cache.row_b;
-            scales[i] = (Off)page * (Off)cache.scale_page_b + slot;
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char *kp, *vp, *ksp, *vsp;
+            if constexpr (SMALL) {      // a lane's keys of K and of V are in one page each
+                const uint64_t page_k = m & 8 ? number[2 * u + 1] : number[2 * u], page_v = c & 2 ? number[2 * u + 1] : number[2 * u];
+                kp = k_head + page_k * cache.page_b;
+                vp = v_head + page_v * cache.page_b;
+                ksp = ks_head + page_k * cache.scale_page_b;
+                vsp = vs_head + page_v * cache.scale_page_b;
+            } else {
+                const uint32_t slot = (uint32_t)(req_tile * kStepTile + 16 * u) & slot_mask;
+                const uint64_t codes = number[u] * (uint64_t)cache.page_b + slot * (uint64_t)cache.row_b;
+                const uint64_t scales = number[u] * (uint64_t)cache.scale_page_b + slot;
+                kp = k_head + codes;
+                vp = v_head + codes;
+                ksp = ks_head + scales;
+                vsp = vs_head + scales;
+            }
+            t.ks[u] = ksp[ks_lane];
+            t.vs[u] = *reinterpret_cast<const uint32_t*>(vsp + vs_lane);
+            t.k[u] = MX_LC(reinterpret_cast<const u32x4*>(kp + k_lane));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.v[4 * u + i] = MX_LC(reinterpret_cast<const uint32_t*>(vp + v_lane[i]));
         }
-        const Off ko = of_group(codes, kg) + k_lane, vo = of_group(codes, vg) + v_lane;
-        const Off kso = of_group(scales, kg) + ks_lane, vso = of_group(scales, vg) + vs_lane;
-        t.ks = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(ks_head + kso));
-        t.vs = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vs_head + vso));
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-            t.k[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k_head + (int64_t)(4 * u) * cache.row_b + ko));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t.v[e] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(v_head + (int64_t)e * cache.row_b + vo));
         if (--req_left == 0) return;
         req_tile += STRIDE;
         if (!SHARED && req_tile == req.tiles) {
@@ -202,7 +219,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     int pos[NT], head[NT], last_vis[NT];      // new token, query head and last key of this lane's rows
     bf16x8 qf[NT][4];
     f32x4 o[NT][8];
-    float m_run[NT], l_run[NT];
+    float m_run[NT], m_use[NT], l_run[NT];      // softmax reference (-inf: no key yet) and what is subtracted, denominators
     auto begin_piece = [&]() {
         const int last = unit.keys - 1;
         piece0 = tile;
@@ -223,7 +240,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
                 qf[nt][t] = __builtin_bit_cast(bf16x8, raw);
             }
             m_run[nt] = -INFINITY;
-            l_run[nt] = 0.f;
+            m_use[nt] = l_run[nt] = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -260,7 +277,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         pair(std::integral_constant<int, 2>{});
         pair(std::integral_constant<int, 3>{});
     };
-    auto scales_of = [](const u32x2& b, float (&sv)[8]) {
+    auto scales_of = [](const uint32_t (&b)[2], float (&sv)[8]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             sv[4 * h] = mx_scale<0>(b[h]);
@@ -277,7 +294,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const float scale = mx_scale_of(t.ks[u] >> (8 * (m & 3)));
+            const float scale = mx_scale_of(t.ks[u]);
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 const bf16x8 kf = __builtin_bit_cast(bf16x8, mx_values(t.k[u][d], scale));
@@ -285,54 +302,58 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
                 for (int nt = 0; nt < NT; ++nt) s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nt][d], s[nt][u], 0, 0, 0);
             }
         }
-        // mask, softmax reference (kept lazily: it moves only for a score more than 2^8 ahead of it), weights
+        // mask, softmax reference, weights
         const bool need_mask = key0 + kStepTile - 1 > min(first_vis, last);
         bf16x8 pp[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (need_mask) {
-                const int lim = last_vis[nt] - key0 - 8 * c;
+                const int lim = last_vis[nt] - key0 - 4 * c;
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (r > lim) s[nt][r >> 2][r & 3] = -INFINITY;
+                    if (16 * (r >> 2) + (r & 3) > lim) s[nt][r >> 2][r & 3] = -INFINITY;
             }
+            // The reference is kept lazily: it moves only for a score more than 2^8 ahead of it, and only then do the four lanes
+            // of a row exchange anything.
             float mx = s[nt][0][0];
 #pragma unroll
             for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[nt][r >> 2][r & 3]);
-            mx = across(mx, [](float x, float y) { return fmaxf(x, y); });
-            const float mx2 = mx * sl2;
-            const float m_new = (mx2 > m_run[nt] + 8.f) ? mx2 : m_run[nt];
-            const float m_use = (m_new == -INFINITY) ? 0.f : m_new;   // a row that has seen no key yet
-            const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - m_use);
-            m_run[nt] = m_new;
+            mx *= sl2;
+            if (__any(mx > m_run[nt] + 8.f)) {
+                mx = across(mx, [](float x, float y) { return fmaxf(x, y); });
+                if (mx > m_run[nt] + 8.f) {
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - mx);
+                    m_run[nt] = m_use[nt] = mx;
+                    l_run[nt] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[nt][j][i] *= alpha;
+                }
+            }
             float rs = 0.f;
             u32x4 packed;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f32x2 x = {__builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1)], sl2, -m_use)),
-                                 __builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sl2, -m_use))};
+                const f32x2 x = {__builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1)], sl2, -m_use[nt])),
+                                 __builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sl2, -m_use[nt]))};
                 rs += x[0] + x[1];      // the denominator from the unrounded weights; for the product they are bf16, as everywhere here
                 packed[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
             }
             pp[nt] = __builtin_bit_cast(bf16x8, packed);
-            l_run[nt] = l_run[nt] * alpha + rs;
-            if (__any(alpha != 1.f)) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nt][j][i] *= alpha;
-            }
+            l_run[nt] += rs;
         }
         // values past the end: zero
-        u32x2 vs = t.vs;
+        uint32_t vs[2] = {t.vs[0], t.vs[1]};
+        auto zero = [&](int e) {
+            t.v[e] = 0u;
+            vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
+        };
+        auto key_of = [&](int e) { return 16 * (e >> 2) + 4 * c + (e & 3); };
         if (key0 + kStepTile > keys) {
-            const int n = keys - key0 - 8 * c;      // of this lane's
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e >= n) {
-                    t.v[e] = 0u;
-                    vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
-                }
+                if (key0 + key_of(e) >= keys) zero(e);
         }
         auto sum_up = [&](int j, const bf16x8& vf) {
 #pragma unroll
@@ -345,42 +366,46 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             uint32_t odd = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if ((vs[e >> 2] >> 8 * (e & 3) & 0xffu) >= 253u && key0 + 8 * c + e > first_vis) odd |= 1u << e;
+                if ((vs[e >> 2] >> 8 * (e & 3) & 0xffu) >= 253u && key0 + key_of(e) > first_vis) odd |= 1u << e;
             if (__any(odd != 0)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint64_t b = __ballot(odd >> e & 1);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (b >> 16 * i & 0xffff) odd_keys |= 1u << (8 * i + e);
+                        if (b >> 16 * i & 0xffff) odd_keys |= 1u << (16 * (e >> 2) + 4 * i + (e & 3));
                 }
                 odd_keys = __builtin_amdgcn_readfirstlane(odd_keys);
-                const uint32_t sv_bytes[2] = {vs[0], vs[1]};
+                // (a key's 16 bytes for the dims of this lane's results are read again: few registers, and seldom)
+                const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)unit.seq * bt.table_len);
+#pragma unroll 1
                 for (uint32_t rest = odd_keys; rest != 0; rest &= rest - 1) {
-                    const int key = __builtin_ctz(rest);
-                    uint32_t v1[8];
-                    float s1[8];
+                    const int key = __builtin_ctz(rest), at_key = key0 + key;
+                    const uint64_t page = min((uint32_t)table[at_key >> cache.log_page], cache.last_page);
+                    const uint32_t slot = (uint32_t)at_key & slot_mask;
+                    const u32x4 codes = *reinterpret_cast<const u32x4*>(v_head + page * cache.page_b + (uint64_t)slot * cache.row_b + 16 * c);
+                    const float scale = mx_scale_of(vs_head[page * cache.scale_page_b + ((uint32_t)c << cache.log_page) + slot]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool it = 8 * c + e == key;
-                        v1[e] = it ? t.v[e] : 0u;
-                        s1[e] = it ? mx_scale_of(sv_bytes[e >> 2] >> 8 * (e & 3) & 0xffu) : 1.f;
-                    }
-                    blocks_of(v1, s1, [&](int j, const bf16x8& vf) {
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const u32x4 two = __builtin_bit_cast(u32x4, pp[nt]);
+                        const uint32_t own = key & 16 ? (key & 2 ? two[3] : two[2]) : (key & 2 ? two[1] : two[0]);
+                        const uint32_t its = (uint32_t)__shfl((int)own, (key >> 2 & 3) * 16 + m);
+                        const float weight = __builtin_bit_cast(float, key & 1 ? its & 0xffff0000u : its << 16);
+                        if (at_key > last_vis[nt]) continue;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                        for (int i = 0; i < 4; ++i) {
+                            const u32x4 x = mx_values(codes[i], scale);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) o[nt][j][i] += key0 + key <= last_vis[nt] ? x[i] : 0.f;
+                            for (int j = 0; j < 4; ++j) {
+                                o[nt][2 * j][i] = fmaf(weight, __builtin_bit_cast(float, x[j] << 16), o[nt][2 * j][i]);
+                                o[nt][2 * j + 1][i] = fmaf(weight, __builtin_bit_cast(float, x[j] & 0xffff0000u), o[nt][2 * j + 1][i]);
+                            }
                         }
-                    });
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (odd_keys >> (8 * c + e) & 1) {
-                        t.v[e] = 0u;
-                        vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
-                    }
+                    if (odd_keys >> key_of(e) & 1) zero(e);
             }
         }
         float sv[8];
@@ -504,14 +529,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             begin_piece();
             return true;
         };
-        static_assert(S >= 2 && S <= 4, "stages are written out");
+        static_assert(S <= 2, "stages are written out");
         for (;;) {
             if (!step(ring[0])) return;
-            if (!step(ring[1])) return;
-            if constexpr (S > 2)
-                if (!step(ring[2])) return;
-            if constexpr (S > 3)
-                if (!step(ring[3])) return;
+            if constexpr (S > 1)
+                if (!step(ring[1])) return;
         }
     }
 }
