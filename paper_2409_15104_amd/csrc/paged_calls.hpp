@@ -59,7 +59,7 @@ struct PagedLayout {
     size_t off_lse, off_prefix, off_work, off_counters, off_splits, bytes;
 };
 constexpr int64_t kPagedSlabs = 1024;    // items' partial results: four for every compute unit
-PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_t total_q) {
+PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_t total_q, int step_rows = 32) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     PagedLayout l;
     l.log_heads = most_log_heads_per_item(shape->n_q_heads, shape->n_kv_heads);
@@ -68,7 +68,7 @@ PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_
     const bool list = total_q * (shape->n_q_heads / shape->n_kv_heads) > kPagedFewRows;
     l.slots = list ? kPagedSlabs / l.units : 0;
     l.capacity = list ? total_q / l.bm + batch + l.slots : 0;
-    const size_t rows = std::max((size_t)cu * kPagedWaves1 * 2 * 32, (size_t)l.slots * l.units * kBM);
+    const size_t rows = std::max((size_t)cu * kPagedWaves1 * 2 * step_rows, (size_t)l.slots * l.units * kBM);
     l.off_lse = rows * kHeadDim * sizeof(float);
     l.off_prefix = up(l.off_lse + rows * sizeof(float));
     l.off_work = up(l.off_prefix + ((size_t)batch + 2) * sizeof(int32_t));
@@ -147,19 +147,20 @@ int append_call(NormRopeParams& p, int to, int page_size, const pec_shape_t* sha
 }
 
 // The merge of spans' pieces: `tokens` workgroups for every sequence and query head.
-void launch_paged_merge(const PagedStepParams& s, int cu, int tokens, int64_t len_k, hipStream_t st) {
+template <class Params>
+void launch_paged_merge(const Params& s, int cu, int tokens, int64_t len_k, hipStream_t st) {
     const int batch = s.a.batch.batch;
     const int64_t rows = (int64_t)batch * tokens, waves_wanted = (int64_t)cu * 8;
     const unsigned heads = (unsigned)s.a.n_q_heads;
     // pieces of the longest unit, as far as the hints tell: a step each at most, and four times a sequence's share of the spans
     const int64_t pieces = std::min({len_k / kStepTile, (int64_t)s.n_spans.d, 4 * (int64_t)s.n_spans.d / batch});
     if (rows * heads >= waves_wanted)
-        hipLaunchKernelGGL(paged_merge_kernel<1>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), heads), dim3(256), 0, st, s,
+        hipLaunchKernelGGL((paged_merge_kernel<1, Params>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), heads), dim3(256), 0, st, s,
                            tokens);
     else if (pieces < 128 || rows * heads > 512)
-        hipLaunchKernelGGL(paged_merge_kernel<4>, dim3((unsigned)rows, heads), dim3(256), 0, st, s, tokens);
+        hipLaunchKernelGGL((paged_merge_kernel<4, Params>), dim3((unsigned)rows, heads), dim3(256), 0, st, s, tokens);
     else
-        hipLaunchKernelGGL(paged_merge_kernel<16>, dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
+        hipLaunchKernelGGL((paged_merge_kernel<16, Params>), dim3((unsigned)rows, heads), dim3(1024), 0, st, s, tokens);
 }
 
 // The work list of sequences with more than few_rows rows per KV head, the pipelined kernel on it, and the merge of its ranges.

@@ -36,6 +36,7 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
     return PEC_OK;
 }
 
+constexpr int kMxStepRows = 48;      // of a slot of a partial result, at most
 // Workspace of pec_attn_paged_mx: pec_attn_paged's, then the area (paged_mx_area_kernel.hpp) of so many pages.
 struct MxLayout {
     PagedLayout paged;
@@ -44,7 +45,7 @@ struct MxLayout {
 MxLayout mx_layout(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t pages) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     MxLayout l;
-    l.paged = paged_layout(compute_units(), shape, batch, total_q);
+    l.paged = paged_layout(compute_units(), shape, batch, total_q, kMxStepRows);
     l.off_area = up(l.paged.bytes);
     l.off_used = up(l.off_area + (size_t)batch * sizeof(int32_t));
     l.off_owner = l.off_used + 256;
@@ -62,13 +63,19 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
     return pages;
 }
 
-// Of row tiles of 16 that a wavefront of paged_mx_step_kernel takes, for sequences of up to so many rows; wavefronts per workgroup.
+// Row tiles of 16 to a unit of paged_mx_step_kernel, for sequences of up to so many rows: what the instructions of a tile of keys cost is
+// about 10 + 3 for each row tile, and every unit pays it.
 #ifndef MX_S
-#define MX_S(nt) 2
+#define MX_S(nt) (nt == 3 ? 1 : 2)
 #endif
-int mx_step_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+int mx_step_tiles(int64_t rows) {
+    int best = 1;
+    for (int nt = 2; nt <= 3; ++nt)
+        if ((rows + 16 * nt - 1) / (16 * nt) * (10 + 3 * nt) < (rows + 16 * best - 1) / (16 * best) * (10 + 3 * best)) best = nt;
+    return best;
+}
 #ifndef MX_W
-#define MX_W(nt) (nt == 4 ? 4 : 8)
+#define MX_W(nt) 8
 #endif
 constexpr int mx_step_waves(int nt) { return MX_W(nt); }
 
@@ -77,12 +84,12 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
              hipStream_t st) {
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
     const int g = p.group, nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
-    PagedStepParams s{};
+    PagedMxStepParams s{};
     s.a = p;
     s.part_out = reinterpret_cast<float*>(ws);
     s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
     s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-    s.cut = StepCut{fast_div(g), nt == 1 ? 4 : nt == 2 ? 5 : 6, p.causal, 0x7fffffff};
+    s.cut = MxCut{fast_div(g), fast_div(16 * nt), p.causal};
     const int waves = cu * waves_per;
     if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
     s.n_spans = fast_div(waves / p.n_kv_heads);
@@ -98,7 +105,7 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
     auto launch_nt = [&](auto is_small) {
         if (nt == 1) launch(std::integral_constant<int, 1>{}, is_small);
         else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_small);
-        else launch(std::integral_constant<int, 4>{}, is_small);
+        else launch(std::integral_constant<int, 3>{}, is_small);
     };
     if (mx.log_page < 4) launch_nt(std::true_type{});
     else launch_nt(std::false_type{});
@@ -197,7 +204,7 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const int cu = std::max(8, compute_units() & ~7), g = p.group;
     if (batch->total_q * g > 0x7fffffff - 64) return PEC_ERR_UNSUPPORTED;      // rows of a KV head
     const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
-    const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
+    const PagedLayout l = mx_layout(shape, batch->batch, batch->total_q, 0).paged;
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
     // sequences with many rows: in the area, if it is there.  `both`: few-row sequences beside them, which stay with their codes;

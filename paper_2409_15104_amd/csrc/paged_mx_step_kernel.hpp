@@ -37,6 +37,28 @@ __device__ __forceinline__ int least_span_mx(int total, int longest, int n_kv_he
     return max(1, (int)__builtin_amdgcn_sqrtf(merge_us * (1.f / 0.6f)));
 }
 
+// How a call's sequences are cut: R = 16, 32 or 48 rows a unit; as StepCut.
+struct MxCut {
+    FastDiv group, rows;
+    int causal;
+    __device__ __forceinline__ int tile_of(int row) const { return rows.div(row); }
+    __device__ __forceinline__ int64_t first_row(int64_t rt) const { return rt * rows.d; }
+    __device__ __forceinline__ int keys(const PagedSeq& s, int rt) const {
+        if (!causal) return s.len_k;
+        const int last_row = min(s.len_q * group.d, (rt + 1) * rows.d) - 1;
+        return max(0, min(s.len_k, s.len_k - s.len_q + group.div(last_row) + 1));
+    }
+    __device__ __forceinline__ int tiles(const PagedSeq& s, int rt) const { return max(1, (keys(s, rt) + kStepTile - 1) / kStepTile); }
+    __device__ __forceinline__ int row_tiles(const PagedSeq& s) const { return rows.div(s.len_q * group.d + rows.d - 1); }
+    __device__ __forceinline__ int all_tiles(const PagedSeq& s) const {
+        const int n = row_tiles(s);
+        int sum = 0;
+        for (int rt = 0; rt < n; ++rt) sum = add_up(sum, tiles(s, rt));
+        return sum;
+    }
+};
+using PagedMxStepParams = PagedStepParamsOf<MxCut>;
+
 struct MxTile {              // 32 keys, as lane (m, c) takes them
     u32x4 k[2];              // dims 32 c ... 32 c + 31 of key 16 u + m
     uint32_t v[8];           // dims 8 m ... 8 m + 7 of keys 16 u + 4 c + i at [4 u + i]
@@ -45,7 +67,7 @@ struct MxTile {              // 32 keys, as lane (m, c) takes them
 
 // SMALL: pages of eight keys.
 template <int NT, int WAVES, int S, bool SHARED, bool SMALL>
-__global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const PagedStepParams p, const PagedMx cache) {
+__global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const PagedMxStepParams p, const PagedMx cache) {
     constexpr int R = 16 * NT;
     constexpr int STRIDE = SHARED ? WAVES : 1;
     __shared__ __attribute__((aligned(1024))) float joint_o[SHARED ? WAVES * 16 * kHeadDim : 1];
@@ -54,7 +76,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, m = lane & 15, c = lane >> 4;
     const int g = p.a.group, causal = p.a.causal;
-    const StepCut& cut = p.cut;
+    const MxCut& cut = p.cut;
     const PagedBatch& bt = p.a.batch;
 
     auto length = [&](const PagedSeq& s) { return SHARED ? cut.row_tiles(s) : cut.all_tiles(s); };
@@ -179,30 +201,36 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     };
     // Keys past the end come along, from the slots behind the last one or from whatever page is at hand: their scores are masked
     // and their values become zeros.
-    auto request = [&](MxTile& t) {
+    const unsigned char *v_base[2], *vs_base[2];      // of the tile whose keys have been requested and whose values have not
+    auto request_k = [&](MxTile& t) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const unsigned char *kp, *vp, *ksp, *vsp;
-            if constexpr (SMALL) {      // a lane's keys of K and of V are in one page each
-                const uint64_t page_k = m & 8 ? number[2 * u + 1] : number[2 * u], page_v = c & 2 ? number[2 * u + 1] : number[2 * u];
-                kp = k_head + page_k * cache.page_b;
-                vp = v_head + page_v * cache.page_b;
-                ksp = ks_head + page_k * cache.scale_page_b;
-                vsp = vs_head + page_v * cache.scale_page_b;
+            const unsigned char *kp, *ksp;
+            if constexpr (SMALL) {      // a lane's keys are in one page, its values' too
+                const uint64_t page = m & 8 ? number[2 * u + 1] : number[2 * u], page_v = c & 2 ? number[2 * u + 1] : number[2 * u];
+                kp = k_head + page * cache.page_b;
+                ksp = ks_head + page * cache.scale_page_b;
+                v_base[u] = v_head + page_v * cache.page_b;
+                vs_base[u] = vs_head + page_v * cache.scale_page_b;
             } else {
                 const uint32_t slot = (uint32_t)(req_tile * kStepTile + 16 * u) & slot_mask;
                 const uint64_t codes = number[u] * (uint64_t)cache.page_b + slot * (uint64_t)cache.row_b;
                 const uint64_t scales = number[u] * (uint64_t)cache.scale_page_b + slot;
                 kp = k_head + codes;
-                vp = v_head + codes;
                 ksp = ks_head + scales;
-                vsp = vs_head + scales;
+                v_base[u] = v_head + codes;
+                vs_base[u] = vs_head + scales;
             }
             t.ks[u] = ksp[ks_lane];
-            t.vs[u] = *reinterpret_cast<const uint32_t*>(vsp + vs_lane);
             t.k[u] = MX_LC(reinterpret_cast<const u32x4*>(kp + k_lane));
+        }
+    };
+    auto request_v = [&](MxTile& t) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t.v[4 * u + i] = MX_LC(reinterpret_cast<const uint32_t*>(vp + v_lane[i]));
+        for (int u = 0; u < 2; ++u) {
+            t.vs[u] = *reinterpret_cast<const uint32_t*>(vs_base[u] + vs_lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.v[4 * u + i] = MX_LC(reinterpret_cast<const uint32_t*>(v_base[u] + v_lane[i]));
         }
         if (--req_left == 0) return;
         req_tile += STRIDE;
@@ -217,7 +245,12 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     const float sl2 = p.a.scale_log2;
     int piece0, end, first_vis;
     int pos[NT], head[NT], last_vis[NT];      // new token, query head and last key of this lane's rows
-    bf16x8 qf[NT][4];
+    // Q as B operands, of more than 32 rows in LDS, in the order in which they are read: registers are short then
+    constexpr bool QLDS = NT > 2;
+    __shared__ u32x4 lds_q[QLDS ? WAVES * NT * 4 * 64 : 1];
+    u32x4* const q_wave = lds_q + (QLDS ? wave * NT * 4 * 64 + lane : 0);
+    u32x4 q_reg[QLDS ? 1 : NT][4];
+    auto q_of = [&](int nt, int t) { return __builtin_bit_cast(bf16x8, QLDS ? q_wave[(nt * 4 + t) * 64] : q_reg[QLDS ? 0 : nt][t]); };
     f32x4 o[NT][8];
     float m_run[NT], m_use[NT], l_run[NT];      // softmax reference (-inf: no key yet) and what is subtracted, denominators
     auto begin_piece = [&]() {
@@ -237,7 +270,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             for (int t = 0; t < 4; ++t) {
                 u32x4 raw = {0u, 0u, 0u, 0u};
                 if (nt * 16 + m < unit.rows) raw = *reinterpret_cast<const u32x4*>(qrow + 8 * t);
-                qf[nt][t] = __builtin_bit_cast(bf16x8, raw);
+                if constexpr (QLDS) q_wave[(nt * 4 + t) * 64] = raw;
+                else q_reg[nt][t] = raw;
             }
             m_run[nt] = -INFINITY;
             m_use[nt] = l_run[nt] = 0.f;
@@ -299,9 +333,10 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             for (int d = 0; d < 4; ++d) {
                 const bf16x8 kf = __builtin_bit_cast(bf16x8, mx_values(t.k[u][d], scale));
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nt][d], s[nt][u], 0, 0, 0);
+                for (int nt = 0; nt < NT; ++nt) s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q_of(nt, d), s[nt][u], 0, 0, 0);
             }
         }
+        if (req_left > 0) request_k(t);
         // mask, softmax reference, weights
         const bool need_mask = key0 + kStepTile - 1 > min(first_vis, last);
         bf16x8 pp[NT];
@@ -411,8 +446,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         float sv[8];
         scales_of(vs, sv);
         blocks_of(t.v, sv, sum_up);
+        if (req_left > 0) request_v(t);
     };
-
     // ---- the unit's result, or the piece's into its slot
     auto finish_piece = [&]() {
         const bool whole = piece0 == 0 && end == unit.tiles;
@@ -448,17 +483,19 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     if (req_left > 0) look_up();
 #pragma unroll
     for (int i = 0; i < S; ++i)
-        if (req_left > 0) request(ring[i]);
+        if (req_left > 0) {
+            request_k(ring[i]);
+            request_v(ring[i]);
+        }
     begin_piece();
     if constexpr (SHARED) {
         auto step = [&](MxTile& t) {
             work(t);
             tile += STRIDE;
-            if (req_left > 0) request(t);
             return --left > 0;
         };
         if (left > 0)
-            while (step(ring[0]) && step(ring[1])) {}
+            while (step(ring[0]) && (S == 1 || step(ring[S - 1]))) {}
         // ---- the wavefronts' results of every row are joined, 16 rows at a time.  O goes to LDS in 16-byte chunks of 4 dims,
         // chunk ch of row r at slot ch * 16 + (r ^ ch % 16): writers (a row per lane) and readers (a chunk per lane, so that a row leaves
         // as one run) touch all banks evenly.
@@ -520,7 +557,6 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             work(t);
             --left;
             ++tile;
-            if (req_left > 0) request(t);
             if (tile < end) return true;
             finish_piece();
             if (left <= 0) return false;

@@ -46,6 +46,8 @@ __device__ __forceinline__ int add_up(int x, int y) { return (int)min((uint32_t)
 struct StepCut {
     FastDiv group;
     int log_r, causal, most_rows;
+    __device__ __forceinline__ int tile_of(int row) const { return row >> log_r; }
+    __device__ __forceinline__ int64_t first_row(int64_t rt) const { return rt << log_r; }
     // keys that row tile `rt` of `s` walks, its steps (tiles of 32 keys, at least one), row tiles of s, steps of all of them
     __device__ __forceinline__ int keys(const PagedSeq& s, int rt) const {
         if (!causal) return s.len_k;
@@ -64,7 +66,8 @@ struct StepCut {
         return sum;
     }
 };
-struct PagedStepParams {
+template <class Cut>
+struct PagedStepParamsOf {
     PagedAttnParams a;
     float* part_out;          // [spans][KV heads][2][32 NT][128]
     float* part_lse;          // [spans][KV heads][2][32 NT]
@@ -72,8 +75,9 @@ struct PagedStepParams {
     FastDiv n_spans;          // of a KV head
     FastDiv kv_heads;
     int32_t unit_rows;        // rows of a unit, as far as the host knows
-    StepCut cut;              // most_rows: sequences with more rows are not this launch's (0x7fffffff: all are)
+    Cut cut;                  // most_rows: sequences with more rows are not this launch's (0x7fffffff: all are)
 };
+using PagedStepParams = PagedStepParamsOf<StepCut>;
 __device__ __forceinline__ int wave_prefix(int x) {      // inclusive
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -674,13 +678,13 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
 // pieces requested at once.  WAVES wavefronts share a row (a new token of a query head): one where there are rows for every
 // wavefront of the chip, which leaves no barrier between them, four or sixteen where there are fewer and more pieces each.
 // `tokens`: workgroups per sequence and query head (times four for WAVES = 1), which share its new tokens.
-template <int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_kernel(const PagedStepParams p, int tokens) {
+template <int WAVES, class Params>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_kernel(const Params p, int tokens) {
     constexpr int N = 2 * WAVES, AHEAD = 4;
     __shared__ __attribute__((aligned(16))) float red[N][kHeadDim];
     __shared__ float red_mx[N], red_den[N];
     const PagedBatch& bt = p.a.batch;
-    const int g = p.a.group, head = blockIdx.y, kvh = p.cut.group.div(head), in_group = head - kvh * g, log_r = p.cut.log_r;
+    const int g = p.a.group, head = blockIdx.y, kvh = p.cut.group.div(head), in_group = head - kvh * g;
     const int grp = (int)(threadIdx.x >> 5) % N, c = threadIdx.x & 31;
     const int per_head = p.prefix[bt.batch], least = p.prefix[bt.batch + 1];
     constexpr int PER_GROUP = WAVES == 1 ? 4 : 1;       // rows a workgroup works on at a time
@@ -693,10 +697,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
         int rt = 0, at = before;       // the row tile in hand, and its first step
         for (int pos = x % tokens; pos < s.len_q; pos += tokens) {
             const int flat = pos * g + in_group;
-            for (; rt < flat >> log_r; ++rt) at += p.cut.tiles(s, rt);
+            for (; rt < p.cut.tile_of(flat); ++rt) at += p.cut.tiles(s, rt);
             const int w0 = spans.of(at), w1 = spans.of(at + p.cut.tiles(s, rt) - 1);
             if (w0 == w1) continue;
-            const int row = flat - (rt << log_r);
+            const int row = flat - (int)p.cut.first_row(rt);
             float mx = -INFINITY, den = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             for (int w = w0 + grp; w <= w1; w += AHEAD * N) {
@@ -708,7 +712,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
                     o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if (w + i * N <= w1) {
                         const int64_t slot = ((int64_t)(w + i * N) * p.a.n_kv_heads + kvh) * 2 + (w + i * N == w0 ? 1 : 0);
-                        const int64_t slot_row = (slot << log_r) + row;
+                        const int64_t slot_row = p.cut.first_row(slot) + row;
                         l[i] = p.part_lse[slot_row];
                         o[i] = *reinterpret_cast<const f32x4*>(p.part_out + slot_row * kHeadDim + 4 * c);
                     }
