@@ -59,7 +59,8 @@ struct PagedLayout {
     size_t off_lse, off_prefix, off_work, off_counters, off_splits, bytes;
 };
 constexpr int64_t kPagedSlabs = 1024;    // items' partial results: four for every compute unit
-PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_t total_q, int step_rows = 32) {
+size_t paged_step_rows(int cu) { return (size_t)cu * kPagedWaves1 * 2 * 32; }      // of all spans' slots
+PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_t total_q, size_t step_rows) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     PagedLayout l;
     l.log_heads = most_log_heads_per_item(shape->n_q_heads, shape->n_kv_heads);
@@ -68,7 +69,7 @@ PagedLayout paged_layout(int cu, const pec_shape_t* shape, int32_t batch, int64_
     const bool list = total_q * (shape->n_q_heads / shape->n_kv_heads) > kPagedFewRows;
     l.slots = list ? kPagedSlabs / l.units : 0;
     l.capacity = list ? total_q / l.bm + batch + l.slots : 0;
-    const size_t rows = std::max((size_t)cu * kPagedWaves1 * 2 * step_rows, (size_t)l.slots * l.units * kBM);
+    const size_t rows = std::max(step_rows, (size_t)l.slots * l.units * kBM);
     l.off_lse = rows * kHeadDim * sizeof(float);
     l.off_prefix = up(l.off_lse + rows * sizeof(float));
     l.off_work = up(l.off_prefix + ((size_t)batch + 2) * sizeof(int32_t));
@@ -267,7 +268,7 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
 size_t pec_paged_workspace_bytes(const pec_shape_t* shape, int32_t batch, int64_t total_q) {
     if (!shape || shape->n_q_heads <= 0 || shape->n_kv_heads <= 0 || batch < 0 || total_q < 0) return 0;
     if (shape->n_q_heads % shape->n_kv_heads != 0) return 0;
-    return paged_layout(compute_units(), shape, batch, total_q).bytes;
+    return paged_layout(compute_units(), shape, batch, total_q, paged_step_rows(compute_units())).bytes;
 }
 
 int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, const pec_paged_batch_t* batch, const void* q,
@@ -305,7 +306,7 @@ int pec_attn_paged(const pec_shape_t* shape, const pec_paged_cache_t* cache, con
     const int cu = std::max(8, compute_units() & ~7), g = p.group;
     if (batch->total_q * g > 0x7fffffff - 64) return PEC_ERR_UNSUPPORTED;      // rows of a KV head
     const int64_t len_q = batch->max_len_q > 0 ? std::min(batch->max_len_q, batch->total_q) : batch->total_q;
-    const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q);
+    const PagedLayout l = paged_layout(compute_units(), shape, batch->batch, batch->total_q, paged_step_rows(compute_units()));
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
     const PagedCut cut = paged_cut(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k);

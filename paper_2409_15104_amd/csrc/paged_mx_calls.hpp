@@ -36,7 +36,13 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
     return PEC_OK;
 }
 
+#ifndef MX_WAVES
+#define MX_WAVES 4
+#endif
+constexpr int kMxWaves = MX_WAVES;      // of a workgroup of paged_mx_step_kernel
 constexpr int kMxStepRows = 48;      // of a slot of a partial result, at most
+// Workgroups of paged_mx_step_kernel, a span each: two to a compute unit, and at least one for every KV head.
+int mx_step_groups(int cu, int n_kv_heads) { return std::max((cu & ~7) * 8 / kMxWaves, (n_kv_heads + 7) / 8 * 8); }
 // Workspace of pec_attn_paged_mx: pec_attn_paged's, then the area (paged_mx_area_kernel.hpp) of so many pages.
 struct MxLayout {
     PagedLayout paged;
@@ -45,7 +51,7 @@ struct MxLayout {
 MxLayout mx_layout(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t pages) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     MxLayout l;
-    l.paged = paged_layout(compute_units(), shape, batch, total_q, kMxStepRows);
+    l.paged = paged_layout(compute_units(), shape, batch, total_q, (size_t)mx_step_groups(std::max(8, compute_units()), shape->n_kv_heads) * 2 * kMxStepRows);
     l.off_area = up(l.paged.bytes);
     l.off_used = up(l.off_area + (size_t)batch * sizeof(int32_t));
     l.off_owner = l.off_used + 256;
@@ -65,50 +71,39 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
 
 // Row tiles of 16 to a unit of paged_mx_step_kernel, for sequences of up to so many rows: what the instructions of a tile of keys cost is
 // about 10 + 3 for each row tile, and every unit pays it.
-#ifndef MX_S
-#define MX_S(nt) (nt == 3 ? 1 : 2)
-#endif
 int mx_step_tiles(int64_t rows) {
     int best = 1;
     for (int nt = 2; nt <= 3; ++nt)
         if ((rows + 16 * nt - 1) / (16 * nt) * (10 + 3 * nt) < (rows + 16 * best - 1) / (16 * best) * (10 + 3 * best)) best = nt;
     return best;
 }
-#ifndef MX_W
-#define MX_W(nt) 8
-#endif
-constexpr int mx_step_waves(int nt) { return MX_W(nt); }
 
 // The sequences of the call (of its side of the area) straight from their codes: spans and their merge.
 int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
              hipStream_t st) {
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
-    const int g = p.group, nt = mx_step_tiles(len_q * g), waves_per = mx_step_waves(nt);
+    const int g = p.group, nt = mx_step_tiles(len_q * g);
     PagedMxStepParams s{};
     s.a = p;
     s.part_out = reinterpret_cast<float*>(ws);
     s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
     s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
     s.cut = MxCut{fast_div(g), fast_div(16 * nt), p.causal};
-    const int waves = cu * waves_per;
-    if (p.n_kv_heads > waves) return PEC_ERR_UNSUPPORTED;      // a wavefront for every KV head
-    s.n_spans = fast_div(waves / p.n_kv_heads);
+    const int groups = mx_step_groups(cu, p.n_kv_heads);
+    s.n_spans = fast_div(groups / p.n_kv_heads);
     s.kv_heads = fast_div(p.n_kv_heads);
     s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
     const int64_t row_tiles = total_q * g / (16 * nt) + batch;
     if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
-    const dim3 grid((unsigned)cu), threads((unsigned)waves_per * 64);
-    auto launch = [&](auto tiles, auto is_small) {
+    const dim3 grid((unsigned)groups), threads((unsigned)kMxWaves * 64);
+    auto launch = [&](auto tiles) {
         constexpr int NT = decltype(tiles)::value;
-        hipLaunchKernelGGL((paged_mx_step_kernel<NT, mx_step_waves(NT), MX_S(NT), false, decltype(is_small)::value>), grid, threads, 0, st, s, mx);
+        if (mx.log_page < 4) hipLaunchKernelGGL((paged_mx_step_kernel<NT, kMxWaves, false, true>), grid, threads, 0, st, s, mx);
+        else hipLaunchKernelGGL((paged_mx_step_kernel<NT, kMxWaves, false, false>), grid, threads, 0, st, s, mx);
     };
-    auto launch_nt = [&](auto is_small) {
-        if (nt == 1) launch(std::integral_constant<int, 1>{}, is_small);
-        else if (nt == 2) launch(std::integral_constant<int, 2>{}, is_small);
-        else launch(std::integral_constant<int, 3>{}, is_small);
-    };
-    if (mx.log_page < 4) launch_nt(std::true_type{});
-    else launch_nt(std::false_type{});
+    if (nt == 1) launch(std::integral_constant<int, 1>{});
+    else if (nt == 2) launch(std::integral_constant<int, 2>{});
+    else launch(std::integral_constant<int, 3>{});
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
     return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;

@@ -1,10 +1,12 @@
 // Attention over a paged cache in 4 bits for sequences with few new tokens: decode steps, drafted tokens, short chunks (gfx950).
 //
-// The work is shared out as in paged_step_kernel: units of up to R query rows that share a KV head, a line of 32-key tiles for each
-// KV head cut into equal spans, one for every wavefront of the chip, pieces merged by paged_merge_kernel; or, for small calls, a
-// workgroup per unit.  What differs is the tile.  In 4 bits it is 4.25 KiB in the place of 16, so it goes from memory straight to
-// registers, S tiles ahead, with no LDS and no wait but the compiler's; and since a byte now stands for two values, what a
-// wavefront does per byte counts four times as much as there.
+// Units, lines and spans as in paged_step_kernel: a unit is up to R query rows that share a KV head, the units' 32-key tiles are one line
+// for each KV head, cut into equal spans; pieces of units are merged by paged_merge_kernel.  Or, for small calls, a workgroup takes
+// a unit, and nothing is left to merge.  Two things differ.  In 4 bits a tile is 4.25 KiB in the place of 16, so it goes from memory
+// straight to registers, a tile ahead, with no LDS and no wait but the compiler's; and since a byte stands for two values, what
+// is done per tile and what a piece's fp32 result costs count four times as much.  So a span belongs to a workgroup: its
+// wavefronts take the tiles in turn and join their results in LDS, and a quarter as many pieces go through memory (with a span
+// for every wavefront 24 x 5 drafted tokens behind 10,000 wrote and read 47 MB of them beside 280 MB of cache: 111 us).
 //
 // Products are 16 x 16 x 32 (lane l: m = l % 16, c = l / 16; A rows m, B columns m, k-slots 8 c ... 8 c + 7; C column m, rows 4 c + i).
 // Scores, S^T = K Q^T: the contraction runs over dims in any order that K and Q agree on, so lane (m, c) takes dims 32 c ... 32 c + 31
@@ -28,6 +30,9 @@
 #endif
 #ifndef MX_LC
 #define MX_LC(x) __builtin_nontemporal_load(x)
+#endif
+#ifndef MX_SPREAD
+#define MX_SPREAD 8
 #endif
 namespace pec {
 
@@ -65,13 +70,14 @@ struct MxTile {              // 32 keys, as lane (m, c) takes them
     uint32_t ks[2], vs[2];   // the scale byte of key 16 u + m for group c, those of keys 16 u + 4 c ... + 3 for group m / 4
 };
 
-// SMALL: pages of eight keys.
-template <int NT, int WAVES, int S, bool SHARED, bool SMALL>
-__global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const PagedMxStepParams p, const PagedMx cache) {
+// NT: row tiles of 16 to a unit.  UNITS: a unit to a workgroup, else a span.  SMALL: pages of eight keys.
+template <int NT, int WAVES, bool UNITS, bool SMALL>
+__global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const PagedMxStepParams p, const PagedMx cache) {
     constexpr int R = 16 * NT;
-    constexpr int STRIDE = SHARED ? WAVES : 1;
-    __shared__ __attribute__((aligned(1024))) float joint_o[SHARED ? WAVES * 16 * kHeadDim : 1];
-    __shared__ float joint[SHARED ? 3 * WAVES * 16 : 1];
+    constexpr bool QLDS = NT > 2;
+    __shared__ __attribute__((aligned(1024))) float joint_o[WAVES * 16 * kHeadDim];
+    __shared__ float joint[3 * WAVES * 16];
+    __shared__ u32x4 lds_q[QLDS ? NT * 4 * 64 : 1];
     __shared__ int32_t chunk_sum[kPagedChunks];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, m = lane & 15, c = lane >> 4;
@@ -79,9 +85,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     const MxCut& cut = p.cut;
     const PagedBatch& bt = p.a.batch;
 
-    auto length = [&](const PagedSeq& s) { return SHARED ? cut.row_tiles(s) : cut.all_tiles(s); };
+    auto length = [&](const PagedSeq& s) { return UNITS ? cut.row_tiles(s) : cut.all_tiles(s); };
     PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
-    if (!SHARED && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
+    if (!UNITS && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
         for (int ch = wave, ahead = 0, at = 0; ch < line.n_chunks; ch += WAVES) {
             for (; at < ch; ++at) ahead = add_up(ahead, chunk_sum[at]);
             const int mine = length(line.load(64 * ch + lane)), all = wave_prefix(mine);
@@ -91,7 +97,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     }
     if (line.total == 0 || line.total == kTooMany) return;
     int least = 1;
-    if constexpr (!SHARED) {
+    if constexpr (!UNITS) {
         int longest = line.total / 64;       // (of more than 64 sequences: that many alike)
         if (line.n_chunks <= 1) {
             longest = cut.row_tiles(line.lanes) > 0 ? (line.lanes.len_k + kStepTile - 1) / kStepTile : 0;
@@ -101,8 +107,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         least = __builtin_amdgcn_readfirstlane(least_span_mx(line.total, longest, p.a.n_kv_heads, p.unit_rows));
         if (blockIdx.x == 0 && threadIdx.x == 0) p.prefix[bt.batch + 1] = least;
     }
-    int at, left, kvh, w = 0;               // place on the line, tiles to work on
-    if constexpr (SHARED) {
+    int at, len, kvh, w = 0;                // place on the line, tiles from there on; slots are numbered 2 w, 2 w + 1
+    if constexpr (UNITS) {
         const WorkOrder order(line.total, 1, p.a.n_kv_heads);
         const uint32_t block = blockIdx.y * kUnitsRow + blockIdx.x;
         if ((block >> 3) >= order.count || order.total > (int64_t)gridDim.x * gridDim.y) return;      // (more units than the rows make: as in paged_step_kernel)
@@ -111,14 +117,14 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
         at = __builtin_amdgcn_readfirstlane((int)unit - kvh * line.total);
     } else {
+        // the KV heads of a span on neighbouring workgroups of an XCD, so that token rows of the cache are read together
         const StepSpans spans(line.total, p.n_spans, least);
-        const int group_no = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
-        w = spans.len < 8 ? wave * (int)gridDim.x + (int)blockIdx.x : group_no * WAVES + wave;
+        w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
         const int span = p.kv_heads.div(w);
         kvh = w - span * p.a.n_kv_heads;
         at = spans.start(span);
-        left = span < p.n_spans.d ? spans.start(span + 1) - at : 0;
-        if (left <= 0) return;
+        len = span < p.n_spans.d ? spans.start(span + 1) - at : 0;
+        if (len <= 0) return;
     }
 
     // Row tile `rt` of sequence `seq`; uniform.
@@ -134,7 +140,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         u.row0 = rt * R;
         u.rows = min(R, s.len_q * g - u.row0);
         u.keys = cut.keys(s, rt);
-        u.tiles = max(SHARED ? 0 : 1, (u.keys + kStepTile - 1) / kStepTile);
+        u.tiles = max(1, (u.keys + kStepTile - 1) / kStepTile);
         return u;
     };
     auto next_unit = [&](const Unit& u) {
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         const PagedSeq s = line.seq(seq);
         const int n_rt = cut.row_tiles(s);
         int rt = 0;
-        if constexpr (SHARED) {
+        if constexpr (UNITS) {
             rt = n_rt - 1 - at;              // the longest first
         } else {
             for (; rt < n_rt; ++rt) {
@@ -171,14 +177,20 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         }
         if (rt < 0 || rt >= n_rt) return;    // (never, as above)
         unit = unit_of(s, seq, rt);
-        tile = SHARED ? wave : at;
-        if constexpr (SHARED) left = max(0, (unit.tiles - wave + WAVES - 1) / WAVES);
+        tile = UNITS ? 0 : at;
+        if constexpr (UNITS) len = unit.tiles;
     }
 
-    // ---- requests: the tile after the last requested one, in the same unit or a later one.  Page numbers are scalar loads a
-    // tile ahead (they count against another counter than the tiles).
+    // ---- requests: tile number n of the span is wavefront n % WAVES's.  Each asks for the one after the last that it asked for, in
+    // the same unit or a later one.  Page numbers are scalar loads a tile ahead (they count against another counter than the tiles).
     Unit req = unit;
-    int req_tile = tile, req_left = left;
+    int req_tile = tile + wave, req_left = len - wave;
+    auto settle = [&]() {
+        while (req_tile >= req.tiles) {
+            req_tile -= req.tiles;
+            req = next_unit(req);
+        }
+    };
     const unsigned char* const k_head = cache.k + (int64_t)kvh * cache.head_b;
     const unsigned char* const v_head = cache.v + (int64_t)kvh * cache.head_b;
     const unsigned char* const ks_head = cache.ks + (int64_t)kvh * cache.scale_head_b;
@@ -193,16 +205,18 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
     for (int i = 0; i < 4; ++i) v_lane[i] = (4u * (SMALL ? c & 1 : c) + i) * cache.row_b + 4u * m;
     uint32_t number[SMALL ? 4 : 2];
     auto look_up = [&]() {
-        const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)req.seq * bt.table_len);
+        const ConstInts table = (ConstInts)(uintptr_t)(bt.table_len > 0 ? bt.table + (int64_t)req.seq * bt.table_len : bt.cu_q);      // (without a page: a word to look at)
         constexpr int KEYS = SMALL ? 8 : 16;
 #pragma unroll
         for (int i = 0; i < kStepTile / KEYS; ++i)
-            number[i] = req.keys == 0 ? 0 : min((uint32_t)table[min(req_tile * kStepTile + KEYS * i, req.keys - 1) >> cache.log_page], cache.last_page);
+            number[i] = (uint32_t)table[max(0, min(req_tile * kStepTile + KEYS * i, req.keys - 1)) >> cache.log_page];
     };
     // Keys past the end come along, from the slots behind the last one or from whatever page is at hand: their scores are masked
     // and their values become zeros.
     const unsigned char *v_base[2], *vs_base[2];      // of the tile whose keys have been requested and whose values have not
     auto request_k = [&](MxTile& t) {
+#pragma unroll
+        for (int i = 0; i < (SMALL ? 4 : 2); ++i) number[i] = min(number[i], cache.last_page);      // (here, so that nobody waits for them before)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const unsigned char *kp, *ksp;
@@ -221,62 +235,63 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
                 v_base[u] = v_head + codes;
                 vs_base[u] = vs_head + scales;
             }
-            t.ks[u] = ksp[ks_lane];
             t.k[u] = MX_LC(reinterpret_cast<const u32x4*>(kp + k_lane));
+            t.ks[u] = ksp[ks_lane];
         }
+        if ((req_left -= WAVES) <= 0) return;      // (behind the last one it is asked for over and over)
+        req_tile += WAVES;
+        if (!UNITS) settle();
+        look_up();
     };
     auto request_v = [&](MxTile& t) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            t.vs[u] = *reinterpret_cast<const uint32_t*>(vs_base[u] + vs_lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) t.v[4 * u + i] = MX_LC(reinterpret_cast<const uint32_t*>(v_base[u] + v_lane[i]));
+            t.vs[u] = *reinterpret_cast<const uint32_t*>(vs_base[u] + vs_lane);
         }
-        if (--req_left == 0) return;
-        req_tile += STRIDE;
-        if (!SHARED && req_tile == req.tiles) {
-            req = next_unit(req);
-            req_tile = 0;
-        }
-        look_up();
     };
 
-    // ---- the piece in hand: tiles [piece0, end) of the unit
+    // ---- the piece in hand: tiles [tile, end) of the unit, `done` tiles of the span behind it
     const float sl2 = p.a.scale_log2;
-    int piece0, end, first_vis;
-    int pos[NT], head[NT], last_vis[NT];      // new token, query head and last key of this lane's rows
-    // Q as B operands, of more than 32 rows in LDS, in the order in which they are read: registers are short then
-    constexpr bool QLDS = NT > 2;
-    __shared__ u32x4 lds_q[QLDS ? WAVES * NT * 4 * 64 : 1];
-    u32x4* const q_wave = lds_q + (QLDS ? wave * NT * 4 * 64 + lane : 0);
+    int end, first_vis, done = 0;
+    int last_vis[NT];                         // last key of this lane's rows
+    // Q as B operands, of more than 32 rows in LDS, one copy for the workgroup, in the order in which they are read: registers are short then
     u32x4 q_reg[QLDS ? 1 : NT][4];
-    auto q_of = [&](int nt, int t) { return __builtin_bit_cast(bf16x8, QLDS ? q_wave[(nt * 4 + t) * 64] : q_reg[QLDS ? 0 : nt][t]); };
+    auto q_of = [&](int i, int t) { return __builtin_bit_cast(bf16x8, QLDS ? lds_q[(i * 4 + t) * 64 + lane] : q_reg[QLDS ? 0 : i][t]); };
     f32x4 o[NT][8];
-    float m_run[NT], m_use[NT], l_run[NT];      // softmax reference (-inf: no key yet) and what is subtracted, denominators
+    float m_run[NT], m_use[NT], l_run[NT];    // softmax reference (-inf: no key yet) and what is subtracted, denominators
     auto begin_piece = [&]() {
         const int last = unit.keys - 1;
-        piece0 = tile;
-        end = SHARED ? unit.tiles : min(unit.tiles, tile + left);
+        end = min(unit.tiles, tile + len - done);
         first_vis = causal ? unit.s.len_k - unit.s.len_q + cut.group.div(unit.row0) : last;       // last key of the first row
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = unit.row0 + nt * 16 + m;
-            pos[nt] = cut.group.div(r);
-            head[nt] = kvh * g + r - pos[nt] * g;
-            last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + pos[nt]) : last;
+            const int row = unit.row0 + nt * 16 + m, pos = cut.group.div(row), head = kvh * g + row - pos * g;
+            last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + pos) : last;
             // rows without a query stay zero and are not stored
-            const __bf16* qrow = p.a.q + (unit.s.q0 + pos[nt]) * p.a.q_stride + (int64_t)head[nt] * kHeadDim + 32 * c;
+            const __bf16* qrow = p.a.q + (unit.s.q0 + pos) * p.a.q_stride + (int64_t)head * kHeadDim + 32 * c;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
+                if (QLDS && (nt * 4 + t) % WAVES != wave) continue;
                 u32x4 raw = {0u, 0u, 0u, 0u};
                 if (nt * 16 + m < unit.rows) raw = *reinterpret_cast<const u32x4*>(qrow + 8 * t);
-                if constexpr (QLDS) q_wave[(nt * 4 + t) * 64] = raw;
+                if constexpr (QLDS) lds_q[(nt * 4 + t) * 64 + lane] = raw;
                 else q_reg[nt][t] = raw;
             }
             m_run[nt] = -INFINITY;
             m_use[nt] = l_run[nt] = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if constexpr (QLDS) {
+            __syncthreads();
+        } else {
+            // Q is used here, so that the compiler waits for it here and not in the loop, where its wait would be one for the tiles
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(q_reg[nt][t]));
         }
     };
     auto across = [](float x, auto op) {      // over the four lanes that share a row
@@ -321,11 +336,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
         }
     };
 
-    auto work = [&](MxTile& t) {
-        const int key0 = tile * kStepTile, keys = unit.keys, last = keys - 1;
+    auto work = [&](MxTile& t, int number_of) {
+        const int key0 = number_of * kStepTile, keys = unit.keys, last = keys - 1;
         f32x4 s[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < NT; ++x) s[x][0] = s[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const float scale = mx_scale_of(t.ks[u]);
@@ -333,55 +348,62 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             for (int d = 0; d < 4; ++d) {
                 const bf16x8 kf = __builtin_bit_cast(bf16x8, mx_values(t.k[u][d], scale));
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q_of(nt, d), s[nt][u], 0, 0, 0);
+                for (int x = 0; x < NT; ++x) s[x][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q_of(x, d), s[x][u], 0, 0, 0);
             }
         }
-        if (req_left > 0) request_k(t);
+        request_k(t);
         // mask, softmax reference, weights
         const bool need_mask = key0 + kStepTile - 1 > min(first_vis, last);
         bf16x8 pp[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int x = 0; x < NT; ++x) {
             if (need_mask) {
-                const int lim = last_vis[nt] - key0 - 4 * c;
+                const int lim = last_vis[x] - key0 - 4 * c;
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (16 * (r >> 2) + (r & 3) > lim) s[nt][r >> 2][r & 3] = -INFINITY;
+                    if (16 * (r >> 2) + (r & 3) > lim) s[x][r >> 2][r & 3] = -INFINITY;
             }
             // The reference is kept lazily: it moves only for a score more than 2^8 ahead of it, and only then do the four lanes
             // of a row exchange anything.
-            float mx = s[nt][0][0];
+            float mx = s[x][0][0];
 #pragma unroll
-            for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[nt][r >> 2][r & 3]);
+            for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[x][r >> 2][r & 3]);
             mx *= sl2;
-            if (__any(mx > m_run[nt] + 8.f)) {
-                mx = across(mx, [](float x, float y) { return fmaxf(x, y); });
-                if (mx > m_run[nt] + 8.f) {
-                    const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - mx);
-                    m_run[nt] = m_use[nt] = mx;
-                    l_run[nt] *= alpha;
+            if (__any(mx > m_run[x] + 8.f)) {
+                mx = across(mx, [](float a, float b) { return fmaxf(a, b); });
+                if (mx > m_run[x] + 8.f) {
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[x] - mx);
+                    m_run[x] = m_use[x] = mx;
+                    l_run[x] *= alpha;
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[nt][j][i] *= alpha;
+                        for (int i = 0; i < 4; ++i) o[x][j][i] *= alpha;
                 }
             }
             float rs = 0.f;
             u32x4 packed;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f32x2 x = {__builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1)], sl2, -m_use[nt])),
-                                 __builtin_amdgcn_exp2f(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sl2, -m_use[nt]))};
-                rs += x[0] + x[1];      // the denominator from the unrounded weights; for the product they are bf16, as everywhere here
-                packed[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+                const f32x2 y = {__builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1)], sl2, -m_use[x])),
+                                 __builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1) + 1], sl2, -m_use[x]))};
+                rs += y[0] + y[1];      // the denominator from the unrounded weights; for the product they are bf16, as everywhere here
+                packed[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
             }
-            pp[nt] = __builtin_bit_cast(bf16x8, packed);
-            l_run[nt] += rs;
+            pp[x] = __builtin_bit_cast(bf16x8, packed);
+            l_run[x] += rs;
         }
+        float sv[8];
+        auto sum_up = [&](int j, const bf16x8& vf) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) o[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[x], o[x][j], 0, 0, 0);
+        };
         // values past the end: zero
-        uint32_t vs[2] = {t.vs[0], t.vs[1]};
+        uint32_t v[8], vs[2] = {t.vs[0], t.vs[1]};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = t.v[e];
         auto zero = [&](int e) {
-            t.v[e] = 0u;
+            v[e] = 0u;
             vs[e >> 2] = (vs[e >> 2] & ~(0xffu << 8 * (e & 3))) | 127u << 8 * (e & 3);
         };
         auto key_of = [&](int e) { return 16 * (e >> 2) + 4 * c + (e & 3); };
@@ -390,10 +412,6 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
             for (int e = 0; e < 8; ++e)
                 if (key0 + key_of(e) >= keys) zero(e);
         }
-        auto sum_up = [&](int j, const bf16x8& vf) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[nt], o[nt][j], 0, 0, 0);
-        };
         // A value that some of the rows do not see reaches them as 0 x value, which NaN (and what exceeds bf16) is not.  In tiles
         // with such keys their values are zeroed for the product, and each is added by itself to the rows that see it.
         uint32_t odd_keys = 0;
@@ -421,19 +439,19 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
                     const u32x4 codes = *reinterpret_cast<const u32x4*>(v_head + page * cache.page_b + (uint64_t)slot * cache.row_b + 16 * c);
                     const float scale = mx_scale_of(vs_head[page * cache.scale_page_b + ((uint32_t)c << cache.log_page) + slot]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const u32x4 two = __builtin_bit_cast(u32x4, pp[nt]);
+                    for (int x = 0; x < NT; ++x) {
+                        const u32x4 two = __builtin_bit_cast(u32x4, pp[x]);
                         const uint32_t own = key & 16 ? (key & 2 ? two[3] : two[2]) : (key & 2 ? two[1] : two[0]);
                         const uint32_t its = (uint32_t)__shfl((int)own, (key >> 2 & 3) * 16 + m);
                         const float weight = __builtin_bit_cast(float, key & 1 ? its & 0xffff0000u : its << 16);
-                        if (at_key > last_vis[nt]) continue;
+                        if (at_key > last_vis[x]) continue;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const u32x4 x = mx_values(codes[i], scale);
+                            const u32x4 y = mx_values(codes[i], scale);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                o[nt][2 * j][i] = fmaf(weight, __builtin_bit_cast(float, x[j] << 16), o[nt][2 * j][i]);
-                                o[nt][2 * j + 1][i] = fmaf(weight, __builtin_bit_cast(float, x[j] & 0xffff0000u), o[nt][2 * j + 1][i]);
+                                o[x][2 * j][i] = fmaf(weight, __builtin_bit_cast(float, y[j] << 16), o[x][2 * j][i]);
+                                o[x][2 * j + 1][i] = fmaf(weight, __builtin_bit_cast(float, y[j] & 0xffff0000u), o[x][2 * j + 1][i]);
                             }
                         }
                     }
@@ -443,67 +461,23 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
                     if (odd_keys >> key_of(e) & 1) zero(e);
             }
         }
-        float sv[8];
         scales_of(vs, sv);
-        blocks_of(t.v, sv, sum_up);
-        if (req_left > 0) request_v(t);
+        blocks_of(v, sv, sum_up);
+        request_v(t);
     };
-    // ---- the unit's result, or the piece's into its slot
-    auto finish_piece = [&]() {
+    // ---- a piece's results are joined, 16 rows at a time, and go out, as the unit's or into the piece's slot.  O goes through LDS in 16-byte
+    // chunks of 4 dims, chunk ch of row r at slot ch * 16 + (r ^ ch % 16): writers (a row per lane) and readers (a chunk per lane, so that
+    // a row leaves as one run) touch all banks evenly.
+    float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
+    auto finish_piece = [&](int piece0) {
         const bool whole = piece0 == 0 && end == unit.tiles;
         const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
+        float* const dst = whole ? static_cast<float*>(p.a.out) : p.part_out;
+        const bool f32 = !whole || p.a.out_f32;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const float l_tot = across(l_run[nt], [](float x, float y) { return x + y; });
-            if (nt * 16 + m < unit.rows) {
-                const int token = unit.s.q0 + pos[nt];
-                const bool none = l_tot == 0.f || unit.keys == 0;       // (without keys the values may be anything, and the sums NaN)
-                const float inv = none ? 0.f : 1.f / l_tot;
-                const float lse = none ? -INFINITY : (m_run[nt] + __builtin_amdgcn_logf(l_tot)) * kLn2;     // NaN from NaN weights
-                if (c == 0) {
-                    if (whole) p.a.lse[(int64_t)head[nt] * bt.total_q + token] = lse;
-                    else p.part_lse[slot_row + nt * 16 + m] = lse;
-                }
-                const int64_t row = whole ? (int64_t)token * p.a.n_q_heads + head[nt] : slot_row + nt * 16 + m;
-                float* const dst = whole ? static_cast<float*>(p.a.out) : p.part_out;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x8 x;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = none ? 0.f : o[nt][j][i] * inv;
-                    const int64_t idx = row * kHeadDim + 32 * c + 8 * i;
-                    if (!whole || p.a.out_f32) *reinterpret_cast<f32x8*>(dst + idx) = x;
-                    else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(x, bf16x8);
-                }
-            }
-        }
-    };
-
-    MxTile ring[S];
-    if (req_left > 0) look_up();
-#pragma unroll
-    for (int i = 0; i < S; ++i)
-        if (req_left > 0) {
-            request_k(ring[i]);
-            request_v(ring[i]);
-        }
-    begin_piece();
-    if constexpr (SHARED) {
-        auto step = [&](MxTile& t) {
-            work(t);
-            tile += STRIDE;
-            return --left > 0;
-        };
-        if (left > 0)
-            while (step(ring[0]) && (S == 1 || step(ring[S - 1]))) {}
-        // ---- the wavefronts' results of every row are joined, 16 rows at a time.  O goes to LDS in 16-byte chunks of 4 dims,
-        // chunk ch of row r at slot ch * 16 + (r ^ ch % 16): writers (a row per lane) and readers (a chunk per lane, so that a row leaves
-        // as one run) touch all banks evenly.
-        float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            __syncthreads();
-            const float l_tot = across(l_run[nt], [](float x, float y) { return x + y; });
+            if (nt * 16 >= unit.rows) break;
+            const float l_tot = across(l_run[nt], [](float a, float b) { return a + b; });
             if (c == 0) {
                 join_m[wave * 16 + m] = m_run[nt];
                 join_l[wave * 16 + m] = l_tot;
@@ -512,65 +486,66 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_mx_step_kernel(const Page
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int ch = 8 * c + 2 * i + h;
-                    po[ch * 16 + (m ^ (ch & 15))] = f32x4{o[nt][4 * h][i], o[nt][4 * h + 1][i], o[nt][4 * h + 2][i], o[nt][4 * h + 3][i]};
+                for (int half = 0; half < 2; ++half) {
+                    const int ch = 8 * c + 2 * i + half;
+                    po[ch * 16 + (m ^ (ch & 15))] = f32x4{o[nt][4 * half][i], o[nt][4 * half + 1][i], o[nt][4 * half + 2][i], o[nt][4 * half + 3][i]};
                 }
             __syncthreads();
             if (threadIdx.x < WAVES * 16) {   // one thread per (row, wavefront): the wavefront's weight
-                const int r = threadIdx.x & 15, k = threadIdx.x >> 4;
+                const int row = threadIdx.x & 15, k = threadIdx.x >> 4;
                 float mx = -INFINITY, den = 0.f;
 #pragma unroll
-                for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, join_m[i * 16 + r]);
+                for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, join_m[i * 16 + row]);
                 const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-                for (int i = 0; i < WAVES; ++i) den += join_l[i * 16 + r] * __builtin_amdgcn_exp2f(join_m[i * 16 + r] - ref);
+                for (int i = 0; i < WAVES; ++i) den += join_l[i * 16 + row] * __builtin_amdgcn_exp2f(join_m[i * 16 + row] - ref);
                 const float inv = den == 0.f ? 0.f : 1.f / den;
-                join_w[k * 16 + r] = __builtin_amdgcn_exp2f(join_m[k * 16 + r] - ref) * inv;
-                const int flat = unit.row0 + nt * 16 + r, at_pos = cut.group.div(flat);
-                if (k == 0 && nt * 16 + r < unit.rows)
-                    p.a.lse[(int64_t)(kvh * g + flat - at_pos * g) * bt.total_q + unit.s.q0 + at_pos] =
-                        den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
+                join_w[k * 16 + row] = __builtin_amdgcn_exp2f(join_m[k * 16 + row] - ref) * inv;
+                if (k == 0 && nt * 16 + row < unit.rows) {
+                    const int flat = unit.row0 + nt * 16 + row, pos = cut.group.div(flat);
+                    float* const to = whole ? p.a.lse + (int64_t)(kvh * g + flat - pos * g) * bt.total_q + unit.s.q0 + pos : p.part_lse + slot_row + nt * 16 + row;
+                    *to = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
+                }
             }
             __syncthreads();
             const int ch = threadIdx.x & 31;
 #pragma unroll
             for (int pass = 0; pass < 8 / WAVES; ++pass) {
-                const int r = pass * 2 * WAVES + (threadIdx.x >> 5), flat = unit.row0 + nt * 16 + r, at_pos = cut.group.div(flat);
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                const int row = pass * 2 * WAVES + (threadIdx.x >> 5), flat = unit.row0 + nt * 16 + row, pos = cut.group.div(flat);
+                f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < WAVES; ++k) {
-                    const float wgt = join_w[k * 16 + r];
-                    const f32x4 y = reinterpret_cast<const f32x4*>(joint_o)[k * 512 + ch * 16 + (r ^ (ch & 15))];
+                    const float wgt = join_w[k * 16 + row];
+                    const f32x4 y = reinterpret_cast<const f32x4*>(joint_o)[k * 512 + ch * 16 + (row ^ (ch & 15))];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = fmaf(wgt, y[i], x[i]);
+                    for (int i = 0; i < 4; ++i) z[i] = fmaf(wgt, y[i], z[i]);
                 }
-                if (nt * 16 + r < unit.rows) {
-                    const int64_t idx = ((int64_t)(unit.s.q0 + at_pos) * p.a.n_q_heads + kvh * g + flat - at_pos * g) * kHeadDim + 4 * ch;
-                    if (p.a.out_f32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.a.out) + idx) = x;
-                    else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(x, bf16x4);
+                if (nt * 16 + row < unit.rows) {
+                    const int64_t to = whole ? (int64_t)(unit.s.q0 + pos) * p.a.n_q_heads + kvh * g + flat - pos * g : slot_row + nt * 16 + row;
+                    if (f32) *reinterpret_cast<f32x4*>(dst + to * kHeadDim + 4 * ch) = z;
+                    else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + to * kHeadDim + 4 * ch) = __builtin_convertvector(z, bf16x4);
                 }
             }
+            __syncthreads();      // before the next 16 rows, or the next piece's, go there
         }
-    } else {
-        auto step = [&](MxTile& t) {      // false: the span has ended
-            work(t);
-            --left;
-            ++tile;
-            if (tile < end) return true;
-            finish_piece();
-            if (left <= 0) return false;
-            unit = next_unit(unit);
-            tile = 0;
-            begin_piece();
-            return true;
-        };
-        static_assert(S <= 2, "stages are written out");
-        for (;;) {
-            if (!step(ring[0])) return;
-            if constexpr (S > 1)
-                if (!step(ring[1])) return;
-        }
+    };
+
+    MxTile t;
+    if (req_left > 0) {
+        if (!UNITS) settle();
+        look_up();
+        request_k(t);
+        request_v(t);
+    }
+    for (;;) {
+        begin_piece();
+        const int piece0 = tile;
+        for (int n = tile + ((wave - done) & (WAVES - 1)); n < end; n += WAVES) work(t, n);
+        finish_piece(piece0);
+        done += end - piece0;
+        if (UNITS || done >= len) return;
+        unit = next_unit(unit);
+        tile = 0;
     }
 }
 
