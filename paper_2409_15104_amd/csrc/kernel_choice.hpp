@@ -403,6 +403,33 @@ inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, 
     return c;
 }
 
+// How paged_mx_step_kernel cuts a call on a cache in 4 bits.  nt: row tiles of 16 to a unit; what the instructions of a tile of keys cost is
+// about 10 + 3 for each of them, and every unit pays it.  units: a workgroup of `waves` wavefronts for every unit, and no merge; else equal
+// spans.  As in paged_cut() the host knows only the longest sequence.  In units the call takes that one's walk, whatever the
+// others hold; in spans 11 us for both launches and what the tiles take together, a sixth of which is counted where there are
+// several sequences, as if they differed as the prompts of a trace do.  (Us as spans / as units, 32 / 8 heads by heads: 4 of 540
+// 11.8 / 8.1, 16 of 1,280 17.2 / 12.3, 64 of 510 20.0 / 11.5, 64 of 1,020 24.8 / 18.1, 128 of 510 34.3 / 20.6; 64 of 27 ... 8,400,
+// 1,560 on the mean, 33.6 / 77.)
+struct MxPlan {
+    int nt, waves;
+    bool units;
+};
+inline MxPlan mx_plan(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+    MxPlan p{1, 4, false};
+    const int64_t rows = len_q * group;
+    auto cost = [&](int nt) { return (rows + 16 * nt - 1) / (16 * nt) * (10 + 3 * nt); };
+    for (int nt = 2; nt <= 3; ++nt)
+        if (cost(nt) < cost(p.nt)) p.nt = nt;
+    const double units = n_kv_heads * (rows <= 16 * p.nt ? (double)batch : (double)total_q * group / (16 * p.nt) + 0.5 * batch);
+    if (units <= cu && p.nt == 1) p.waves = 8;
+    const double slots = cu * 8.0 / p.waves, tiles = len_k / 32.0;
+    const double step = (p.waves == 8 ? 1.0 : 0.72) * (1 + 0.35 * (p.nt - 1)), walk = step * std::ceil(tiles / p.waves);
+    const double as_units = 5.5 + std::max(walk, units / slots * walk);
+    const double as_spans = 11 + units * tiles * 0.19 * (1 + 0.5 * (p.nt - 1)) / cu / (batch == 1 ? 1 : 6);
+    p.units = as_units <= as_spans;
+    return p;
+}
+
 // Wavefronts per token of norm_rope_kernel, each with as many of the token's groups of four head rows as the first (rounded up, so that
 // the last may have fewer or none: 4 groups for 3 wavefronts are 2, 2 and none).
 inline int norm_rope_parts(int cu, int64_t tokens, int64_t quads) {

@@ -36,13 +36,11 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
     return PEC_OK;
 }
 
-#ifndef MX_WAVES
-#define MX_WAVES 4
-#endif
-constexpr int kMxWaves = MX_WAVES;      // of a workgroup of paged_mx_step_kernel
+// Whether neighbouring heads' rows of a token are neighbours in memory: 64 bytes each, half a cache line.
+bool mx_by_token(const PagedMx& mx) { return mx.head_b < mx.row_b; }
 constexpr int kMxStepRows = 48;      // of a slot of a partial result, at most
-// Workgroups of paged_mx_step_kernel, a span each: two to a compute unit, and at least one for every KV head.
-int mx_step_groups(int cu, int n_kv_heads) { return std::max((cu & ~7) * 8 / kMxWaves, (n_kv_heads + 7) / 8 * 8); }
+// Spans of all KV heads: one for every wavefront of eight to a compute unit at most, and one for every head at least.
+int mx_most_spans(int cu, int n_kv_heads) { return std::max((cu & ~7) * 8, (n_kv_heads + 63) / 64 * 64); }
 // Workspace of pec_attn_paged_mx: pec_attn_paged's, then the area (paged_mx_area_kernel.hpp) of so many pages.
 struct MxLayout {
     PagedLayout paged;
@@ -51,7 +49,7 @@ struct MxLayout {
 MxLayout mx_layout(const pec_shape_t* shape, int32_t batch, int64_t total_q, int64_t pages) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     MxLayout l;
-    l.paged = paged_layout(compute_units(), shape, batch, total_q, (size_t)mx_step_groups(std::max(8, compute_units()), shape->n_kv_heads) * 2 * kMxStepRows);
+    l.paged = paged_layout(compute_units(), shape, batch, total_q, (size_t)mx_most_spans(std::max(8, compute_units()), shape->n_kv_heads) * 2 * kMxStepRows);
     l.off_area = up(l.paged.bytes);
     l.off_used = up(l.off_area + (size_t)batch * sizeof(int32_t));
     l.off_owner = l.off_used + 256;
@@ -69,41 +67,68 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
     return pages;
 }
 
-// Row tiles of 16 to a unit of paged_mx_step_kernel, for sequences of up to so many rows: what the instructions of a tile of keys cost is
-// about 10 + 3 for each row tile, and every unit pays it.
-int mx_step_tiles(int64_t rows) {
-    int best = 1;
-    for (int nt = 2; nt <= 3; ++nt)
-        if ((rows + 16 * nt - 1) / (16 * nt) * (10 + 3 * nt) < (rows + 16 * best - 1) / (16 * best) * (10 + 3 * best)) best = nt;
-    return best;
-}
-
 // The sequences of the call (of its side of the area) straight from their codes: spans and their merge.
 int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
              hipStream_t st) {
+    using std::integral_constant;
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
-    const int g = p.group, nt = mx_step_tiles(len_q * g);
+    const int g = p.group;
+    const MxPlan plan = mx_plan(cu, g, p.n_kv_heads, batch, total_q, len_q, len_k);
+    const int nt = plan.nt;
+    const bool small = mx.log_page < 4;
     PagedMxStepParams s{};
     s.a = p;
+    s.cut = MxCut{fast_div(g), fast_div(16 * nt), p.causal};
+    dim3 grid;
+    // WAVES, HEADS: wavefronts to a span or unit, KV heads side by side in a workgroup (paged_mx_step_kernel)
+    auto launch = [&](auto tiles, auto waves, auto heads, auto units, auto pages_of_eight) {
+        constexpr int WAVES = decltype(waves)::value, HEADS = decltype(heads)::value;
+        hipLaunchKernelGGL((paged_mx_step_kernel<decltype(tiles)::value, WAVES, HEADS, decltype(units)::value, decltype(pages_of_eight)::value>),
+                           grid, dim3((unsigned)(HEADS * WAVES) * 64), 0, st, s, mx);
+    };
+    const integral_constant<int, 1> one{};
+    const integral_constant<int, 2> two{};
+    const integral_constant<int, 3> three{};
+    const integral_constant<int, 4> four{};
+    const integral_constant<int, 8> eight{};
+    const std::true_type yes{};
+    const std::false_type no{};
+    if (plan.units && !small) {
+        // two heads to a workgroup where they share cache lines (64 sequences of 510: 17.6 us with one, 11.7 with two)
+        const int heads = nt == 1 && plan.waves == 4 && mx_by_token(mx) && p.n_kv_heads % 2 == 0 ? 2 : 1;
+        s.kv_heads = fast_div(p.n_kv_heads / heads);
+        const int64_t groups = (total_q * g / (16 * nt) + batch) * s.kv_heads.d;
+        if (groups > 0x7fffff00) return PEC_ERR_UNSUPPORTED;
+        grid = dim3((unsigned)std::min<int64_t>((groups + 7) / 8 * 8, kUnitsRow), (unsigned)((groups + kUnitsRow - 1) / kUnitsRow));
+        if (nt == 3) launch(three, four, one, yes, no);
+        else if (nt == 2) launch(two, four, one, yes, no);
+        else if (plan.waves == 8) launch(one, eight, one, yes, no);
+        else if (heads == 2) launch(one, four, two, yes, no);
+        else launch(one, four, one, yes, no);
+        return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;
+    }
     s.part_out = reinterpret_cast<float*>(ws);
     s.part_lse = reinterpret_cast<float*>(ws + l.off_lse);
     s.prefix = reinterpret_cast<int32_t*>(ws + l.off_prefix);
-    s.cut = MxCut{fast_div(g), fast_div(16 * nt), p.causal};
-    const int groups = mx_step_groups(cu, p.n_kv_heads);
-    s.n_spans = fast_div(groups / p.n_kv_heads);
-    s.kv_heads = fast_div(p.n_kv_heads);
+    // Single row tiles, by token: eight heads side by side, a wavefront for each one's span, so that whole token rows are read by one compute
+    // unit at one time (4 x 110,000 tokens, 64 / 8 heads: 106 us, with the heads apart 118 ... 124); else four wavefronts to a
+    // span and two workgroups to a compute unit (the same by heads: 85).
+    const bool side_by_side = nt == 1 && !small && mx_by_token(mx) && p.n_kv_heads % 8 == 0;
+    const int heads = side_by_side ? 8 : 1, lines = p.n_kv_heads / heads;
+    const int groups = std::max(side_by_side ? cu : 2 * cu, (p.n_kv_heads + 63) / 64 * 64 / heads);
+    s.n_spans = fast_div(groups / lines);
+    s.kv_heads = fast_div(lines);
     s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
     const int64_t row_tiles = total_q * g / (16 * nt) + batch;
     if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
-    const dim3 grid((unsigned)groups), threads((unsigned)kMxWaves * 64);
-    auto launch = [&](auto tiles) {
-        constexpr int NT = decltype(tiles)::value;
-        if (mx.log_page < 4) hipLaunchKernelGGL((paged_mx_step_kernel<NT, kMxWaves, false, true>), grid, threads, 0, st, s, mx);
-        else hipLaunchKernelGGL((paged_mx_step_kernel<NT, kMxWaves, false, false>), grid, threads, 0, st, s, mx);
-    };
-    if (nt == 1) launch(std::integral_constant<int, 1>{});
-    else if (nt == 2) launch(std::integral_constant<int, 2>{});
-    else launch(std::integral_constant<int, 3>{});
+    grid = dim3((unsigned)groups);
+    if (side_by_side) launch(one, one, eight, no, no);
+    else if (small && nt == 1) launch(one, four, one, no, yes);
+    else if (small && nt == 2) launch(two, four, one, no, yes);
+    else if (small) launch(three, four, one, no, yes);
+    else if (nt == 1) launch(one, four, one, no, no);
+    else if (nt == 2) launch(two, four, one, no, no);
+    else launch(three, four, one, no, no);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     launch_paged_merge(s, cu, (int)std::max<int64_t>(1, std::min<int64_t>(len_q, 256)), len_k, st);
     return hipGetLastError() == hipSuccess ? PEC_OK : PEC_ERR_HIP;

@@ -25,15 +25,6 @@
 #include "paged_mx_common.hpp"
 #include "paged_step_kernel.hpp"
 
-#ifndef MX_LS
-#define MX_LS(x) __builtin_nontemporal_load(x)
-#endif
-#ifndef MX_LC
-#define MX_LC(x) __builtin_nontemporal_load(x)
-#endif
-#ifndef MX_SPREAD
-#define MX_SPREAD 8
-#endif
 namespace pec {
 
 // Steps that a span should have at least, as least_span(), a step taking its wavefront 0.6 us.
@@ -64,31 +55,36 @@ struct MxCut {
 };
 using PagedMxStepParams = PagedStepParamsOf<MxCut>;
 
+constexpr float kNoKey = -0x1.fffffep127f;
+
 struct MxTile {              // 32 keys, as lane (m, c) takes them
     u32x4 k[2];              // dims 32 c ... 32 c + 31 of key 16 u + m
     uint32_t v[8];           // dims 8 m ... 8 m + 7 of keys 16 u + 4 c + i at [4 u + i]
     uint32_t ks[2], vs[2];   // the scale byte of key 16 u + m for group c, those of keys 16 u + 4 c ... + 3 for group m / 4
 };
 
-// NT: row tiles of 16 to a unit.  UNITS: a unit to a workgroup, else a span.  SMALL: pages of eight keys.
-template <int NT, int WAVES, bool UNITS, bool SMALL>
-__global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const PagedMxStepParams p, const PagedMx cache) {
+// NT: row tiles of 16 to a unit.  WAVES: wavefronts of a span.  HEADS: KV heads whose spans share a workgroup: two where neighbouring
+// heads' rows of a token lie side by side, 64 bytes each, half a cache line, which the compute unit then fetches once.  UNITS: a unit
+// in the place of a span.  SMALL: pages of eight keys.
+template <int NT, int WAVES, int HEADS, bool UNITS, bool SMALL>
+__global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(const PagedMxStepParams p, const PagedMx cache) {
     constexpr int R = 16 * NT;
     constexpr bool QLDS = NT > 2;
-    __shared__ __attribute__((aligned(1024))) float joint_o[WAVES * 16 * kHeadDim];
-    __shared__ float joint[3 * WAVES * 16];
-    __shared__ u32x4 lds_q[QLDS ? NT * 4 * 64 : 1];
+    __shared__ __attribute__((aligned(1024))) float joint_all[HEADS][WAVES > 1 ? WAVES * 16 * kHeadDim : 1];
+    __shared__ float joint_sums[HEADS][3 * WAVES * 16];
+    __shared__ u32x4 lds_q[HEADS][QLDS ? NT * 4 * 64 : 1];
     __shared__ int32_t chunk_sum[kPagedChunks];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, m = lane & 15, c = lane >> 4;
+    const int wave_no = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), side = wave_no / WAVES, wave = wave_no % WAVES;
+    const int lane = threadIdx.x & 63, m = lane & 15, c = lane >> 4, tid = threadIdx.x % (WAVES * 64);
+    float *const joint_o = joint_all[side], *const joint = joint_sums[side];
     const int g = p.a.group, causal = p.a.causal;
     const MxCut& cut = p.cut;
     const PagedBatch& bt = p.a.batch;
 
     auto length = [&](const PagedSeq& s) { return UNITS ? cut.row_tiles(s) : cut.all_tiles(s); };
-    PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
+    PagedLine<HEADS * WAVES, decltype(length)> line(bt, length, chunk_sum, wave_no);
     if (!UNITS && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
-        for (int ch = wave, ahead = 0, at = 0; ch < line.n_chunks; ch += WAVES) {
+        for (int ch = wave_no, ahead = 0, at = 0; ch < line.n_chunks; ch += HEADS * WAVES) {
             for (; at < ch; ++at) ahead = add_up(ahead, chunk_sum[at]);
             const int mine = length(line.load(64 * ch + lane)), all = wave_prefix(mine);
             if (64 * ch + lane < bt.batch) p.prefix[64 * ch + lane] = add_up(ahead, all) - mine;
@@ -109,50 +105,40 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
     }
     int at, len, kvh, w = 0;                // place on the line, tiles from there on; slots are numbered 2 w, 2 w + 1
     if constexpr (UNITS) {
-        const WorkOrder order(line.total, 1, p.a.n_kv_heads);
+        const WorkOrder order(line.total, 1, p.kv_heads.d);
         const uint32_t block = blockIdx.y * kUnitsRow + blockIdx.x;
         if ((block >> 3) >= order.count || order.total > (int64_t)gridDim.x * gridDim.y) return;      // (more units than the rows make: as in paged_step_kernel)
         const int64_t unit = order.unit(block & 7, block >> 3);
         if (unit < 0) return;
         kvh = __builtin_amdgcn_readfirstlane((int)unit / line.total);
         at = __builtin_amdgcn_readfirstlane((int)unit - kvh * line.total);
+        kvh = kvh * HEADS + side;
     } else {
         // the KV heads of a span on neighbouring workgroups of an XCD, so that token rows of the cache are read together
         const StepSpans spans(line.total, p.n_spans, least);
         w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
         const int span = p.kv_heads.div(w);
-        kvh = w - span * p.a.n_kv_heads;
+        kvh = (w - span * p.kv_heads.d) * HEADS + side;
+        w = span * p.a.n_kv_heads + kvh;
         at = spans.start(span);
         len = span < p.n_spans.d ? spans.start(span + 1) - at : 0;
         if (len <= 0) return;
     }
 
-    // Row tile `rt` of sequence `seq`; uniform.
+    // Row tile `rt` of sequence `seq`; uniform.  (The sequence itself is looked up where it is needed: scalar registers are short.)
     struct Unit {
-        PagedSeq s;
-        int seq, rt, row0, rows, keys, tiles;
+        int seq, rt, keys, tiles;
     };
     auto unit_of = [&](const PagedSeq& s, int seq, int rt) {
-        Unit u;
-        u.s = s;
-        u.seq = seq;
-        u.rt = rt;
-        u.row0 = rt * R;
-        u.rows = min(R, s.len_q * g - u.row0);
-        u.keys = cut.keys(s, rt);
-        u.tiles = max(1, (u.keys + kStepTile - 1) / kStepTile);
-        return u;
+        const int keys = cut.keys(s, rt);
+        return Unit{seq, rt, keys, max(1, (keys + kStepTile - 1) / kStepTile)};
     };
     auto next_unit = [&](const Unit& u) {
-        PagedSeq s = u.s;
         int seq = u.seq, rt = u.rt + 1;
+        PagedSeq s = line.seq(seq);
         while (rt >= cut.row_tiles(s)) {
             rt = 0;
-            if (++seq >= bt.batch) {       // (never, unless the offsets change under the launch: what is left has no rows and no keys)
-                seq = 0;
-                s = PagedSeq{0, 0, 0};
-                break;
-            }
+            if (++seq >= bt.batch) return Unit{0, 0, 0, 1};       // (never, unless the offsets change under the launch)
             s = line.seq(seq);
         }
         return unit_of(s, seq, rt);
@@ -203,6 +189,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
     uint32_t v_lane[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v_lane[i] = (4u * (SMALL ? c & 1 : c) + i) * cache.row_b + 4u * m;
+    // Codes that no other wavefront wants are marked as read once; half a cache line is left for the neighbouring head's.
+    auto code_load = [](auto* from) {
+        if constexpr (HEADS > 1) return *from;
+        else return __builtin_nontemporal_load(from);
+    };
     uint32_t number[SMALL ? 4 : 2];
     auto look_up = [&]() {
         const ConstInts table = (ConstInts)(uintptr_t)(bt.table_len > 0 ? bt.table + (int64_t)req.seq * bt.table_len : bt.cu_q);      // (without a page: a word to look at)
@@ -235,7 +226,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
                 v_base[u] = v_head + codes;
                 vs_base[u] = vs_head + scales;
             }
-            t.k[u] = MX_LC(reinterpret_cast<const u32x4*>(kp + k_lane));
+            t.k[u] = code_load(reinterpret_cast<const u32x4*>(kp + k_lane));
             t.ks[u] = ksp[ks_lane];
         }
         if ((req_left -= WAVES) <= 0) return;      // (behind the last one it is asked for over and over)
@@ -247,40 +238,43 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t.v[4 * u + i] = MX_LC(reinterpret_cast<const uint32_t*>(v_base[u] + v_lane[i]));
+            for (int i = 0; i < 4; ++i) t.v[4 * u + i] = code_load(reinterpret_cast<const uint32_t*>(v_base[u] + v_lane[i]));
             t.vs[u] = *reinterpret_cast<const uint32_t*>(vs_base[u] + vs_lane);
         }
     };
 
     // ---- the piece in hand: tiles [tile, end) of the unit, `done` tiles of the span behind it
     const float sl2 = p.a.scale_log2;
-    int end, first_vis, done = 0;
+    int end, first_vis, done = 0, q0, rows;   // (q0, rows: the unit's sequence begins there, and so many rows are its)
     int last_vis[NT];                         // last key of this lane's rows
     // Q as B operands, of more than 32 rows in LDS, one copy for the workgroup, in the order in which they are read: registers are short then
     u32x4 q_reg[QLDS ? 1 : NT][4];
-    auto q_of = [&](int i, int t) { return __builtin_bit_cast(bf16x8, QLDS ? lds_q[(i * 4 + t) * 64 + lane] : q_reg[QLDS ? 0 : i][t]); };
+    auto q_of = [&](int i, int t) { return __builtin_bit_cast(bf16x8, QLDS ? lds_q[side][(i * 4 + t) * 64 + lane] : q_reg[QLDS ? 0 : i][t]); };
     f32x4 o[NT][8];
-    float m_run[NT], m_use[NT], l_run[NT];    // softmax reference (-inf: no key yet) and what is subtracted, denominators
+    float m_run[NT], l_run[NT];    // softmax reference (kNoKey: no key yet; finite, so that it can be subtracted), denominators
     auto begin_piece = [&]() {
-        const int last = unit.keys - 1;
+        const int last = unit.keys - 1, row0 = unit.rt * R;
+        const PagedSeq seq = line.seq(unit.seq);
+        q0 = seq.q0;
+        rows = min(R, seq.len_q * g - row0);
         end = min(unit.tiles, tile + len - done);
-        first_vis = causal ? unit.s.len_k - unit.s.len_q + cut.group.div(unit.row0) : last;       // last key of the first row
+        first_vis = causal ? seq.len_k - seq.len_q + cut.group.div(row0) : last;       // last key of the first row
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = unit.row0 + nt * 16 + m, pos = cut.group.div(row), head = kvh * g + row - pos * g;
-            last_vis[nt] = causal ? min(last, unit.s.len_k - unit.s.len_q + pos) : last;
+            const int row = row0 + nt * 16 + m, pos = cut.group.div(row), head = kvh * g + row - pos * g;
+            last_vis[nt] = causal ? min(last, seq.len_k - seq.len_q + pos) : last;
             // rows without a query stay zero and are not stored
-            const __bf16* qrow = p.a.q + (unit.s.q0 + pos) * p.a.q_stride + (int64_t)head * kHeadDim + 32 * c;
+            const __bf16* qrow = p.a.q + (q0 + pos) * p.a.q_stride + (int64_t)head * kHeadDim + 32 * c;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 if (QLDS && (nt * 4 + t) % WAVES != wave) continue;
                 u32x4 raw = {0u, 0u, 0u, 0u};
-                if (nt * 16 + m < unit.rows) raw = *reinterpret_cast<const u32x4*>(qrow + 8 * t);
-                if constexpr (QLDS) lds_q[(nt * 4 + t) * 64 + lane] = raw;
+                if (nt * 16 + m < rows) raw = *reinterpret_cast<const u32x4*>(qrow + 8 * t);
+                if constexpr (QLDS) lds_q[side][(nt * 4 + t) * 64 + lane] = raw;
                 else q_reg[nt][t] = raw;
             }
-            m_run[nt] = -INFINITY;
-            m_use[nt] = l_run[nt] = 0.f;
+            m_run[nt] = kNoKey;
+            l_run[nt] = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -373,7 +367,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
                 mx = across(mx, [](float a, float b) { return fmaxf(a, b); });
                 if (mx > m_run[x] + 8.f) {
                     const float alpha = __builtin_amdgcn_exp2f(m_run[x] - mx);
-                    m_run[x] = m_use[x] = mx;
+                    m_run[x] = mx;
                     l_run[x] *= alpha;
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -385,8 +379,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
             u32x4 packed;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f32x2 y = {__builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1)], sl2, -m_use[x])),
-                                 __builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1) + 1], sl2, -m_use[x]))};
+                const f32x2 y = {__builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1)], sl2, -m_run[x])),
+                                 __builtin_amdgcn_exp2f(fmaf(s[x][e >> 1][2 * (e & 1) + 1], sl2, -m_run[x]))};
                 rs += y[0] + y[1];      // the denominator from the unrounded weights; for the product they are bf16, as everywhere here
                 packed[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
             }
@@ -471,13 +465,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
     float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
     auto finish_piece = [&](int piece0) {
         const bool whole = piece0 == 0 && end == unit.tiles;
+        const int row0 = unit.rt * R;
         const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
         float* const dst = whole ? static_cast<float*>(p.a.out) : p.part_out;
         const bool f32 = !whole || p.a.out_f32;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (nt * 16 >= unit.rows) break;
+            if (nt * 16 >= rows) break;
             const float l_tot = across(l_run[nt], [](float a, float b) { return a + b; });
+            if constexpr (WAVES == 1) {      // nobody to join
+                const int flat = row0 + nt * 16 + m, pos = cut.group.div(flat), head = kvh * g + flat - pos * g, token = q0 + pos;
+                if (nt * 16 + m >= rows) continue;
+                const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+                float* const to = whole ? p.a.lse + (int64_t)head * bt.total_q + token : p.part_lse + slot_row + nt * 16 + m;
+                if (c == 0) *to = l_tot == 0.f ? -INFINITY : (m_run[nt] + __builtin_amdgcn_logf(l_tot)) * kLn2;      // NaN from NaN weights
+                const int64_t row = whole ? (int64_t)token * p.a.n_q_heads + head : slot_row + nt * 16 + m;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x8 y;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = o[nt][j][i] * inv;
+                    const int64_t idx = row * kHeadDim + 32 * c + 8 * i;
+                    if (f32) *reinterpret_cast<f32x8*>(dst + idx) = y;
+                    else *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.a.out) + idx) = __builtin_convertvector(y, bf16x8);
+                }
+                continue;
+            }
             if (c == 0) {
                 join_m[wave * 16 + m] = m_run[nt];
                 join_l[wave * 16 + m] = l_tot;
@@ -491,27 +504,26 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
                     po[ch * 16 + (m ^ (ch & 15))] = f32x4{o[nt][4 * half][i], o[nt][4 * half + 1][i], o[nt][4 * half + 2][i], o[nt][4 * half + 3][i]};
                 }
             __syncthreads();
-            if (threadIdx.x < WAVES * 16) {   // one thread per (row, wavefront): the wavefront's weight
-                const int row = threadIdx.x & 15, k = threadIdx.x >> 4;
-                float mx = -INFINITY, den = 0.f;
+            if (tid < WAVES * 16) {   // one thread per (row, wavefront): the wavefront's weight
+                const int row = tid & 15, k = tid >> 4;
+                float mx = kNoKey, den = 0.f;
 #pragma unroll
                 for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, join_m[i * 16 + row]);
-                const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-                for (int i = 0; i < WAVES; ++i) den += join_l[i * 16 + row] * __builtin_amdgcn_exp2f(join_m[i * 16 + row] - ref);
+                for (int i = 0; i < WAVES; ++i) den += join_l[i * 16 + row] * __builtin_amdgcn_exp2f(join_m[i * 16 + row] - mx);
                 const float inv = den == 0.f ? 0.f : 1.f / den;
-                join_w[k * 16 + row] = __builtin_amdgcn_exp2f(join_m[k * 16 + row] - ref) * inv;
-                if (k == 0 && nt * 16 + row < unit.rows) {
-                    const int flat = unit.row0 + nt * 16 + row, pos = cut.group.div(flat);
-                    float* const to = whole ? p.a.lse + (int64_t)(kvh * g + flat - pos * g) * bt.total_q + unit.s.q0 + pos : p.part_lse + slot_row + nt * 16 + row;
+                join_w[k * 16 + row] = __builtin_amdgcn_exp2f(join_m[k * 16 + row] - mx) * inv;
+                if (k == 0 && nt * 16 + row < rows) {
+                    const int flat = row0 + nt * 16 + row, pos = cut.group.div(flat);
+                    float* const to = whole ? p.a.lse + (int64_t)(kvh * g + flat - pos * g) * bt.total_q + q0 + pos : p.part_lse + slot_row + nt * 16 + row;
                     *to = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
                 }
             }
             __syncthreads();
-            const int ch = threadIdx.x & 31;
+            const int ch = tid & 31;
 #pragma unroll
             for (int pass = 0; pass < 8 / WAVES; ++pass) {
-                const int row = pass * 2 * WAVES + (threadIdx.x >> 5), flat = unit.row0 + nt * 16 + row, pos = cut.group.div(flat);
+                const int row = pass * 2 * WAVES + (tid >> 5), flat = row0 + nt * 16 + row, pos = cut.group.div(flat);
                 f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < WAVES; ++k) {
@@ -520,8 +532,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_mx_step_kernel(const Page
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[i] = fmaf(wgt, y[i], z[i]);
                 }
-                if (nt * 16 + row < unit.rows) {
-                    const int64_t to = whole ? (int64_t)(unit.s.q0 + pos) * p.a.n_q_heads + kvh * g + flat - pos * g : slot_row + nt * 16 + row;
+                if (nt * 16 + row < rows) {
+                    const int64_t to = whole ? (int64_t)(q0 + pos) * p.a.n_q_heads + kvh * g + flat - pos * g : slot_row + nt * 16 + row;
                     if (f32) *reinterpret_cast<f32x4*>(dst + to * kHeadDim + 4 * ch) = z;
                     else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + to * kHeadDim + 4 * ch) = __builtin_convertvector(z, bf16x4);
                 }
