@@ -403,30 +403,42 @@ inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, 
     return c;
 }
 
-// How paged_mx_step_kernel cuts a call on a cache in 4 bits.  nt: row tiles of 16 to a unit; what the instructions of a tile of keys cost is
-// about 10 + 3 for each of them, and every unit pays it.  units: a workgroup of `waves` wavefronts for every unit, and no merge; else equal
-// spans.  As in paged_cut() the host knows only the longest sequence.  In units the call takes that one's walk, whatever the
-// others hold; in spans 11 us for both launches and what the tiles take together, a sixth of which is counted where there are
-// several sequences, as if they differed as the prompts of a trace do.  (Us as spans / as units, 32 / 8 heads by heads: 4 of 540
-// 11.8 / 8.1, 16 of 1,280 17.2 / 12.3, 64 of 510 20.0 / 11.5, 64 of 1,020 24.8 / 18.1, 128 of 510 34.3 / 20.6; 64 of 27 ... 8,400,
-// 1,560 on the mean, 33.6 / 77.)
+// How a call on a cache in 4 bits is cut.  paged_mx_step_kernel, straight from the codes: nt row tiles of 16 to a unit (what the
+// instructions of a tile of keys cost is about 10 + 3 for each of them, and every unit pays it); `units`: a workgroup of `waves` wavefronts
+// for every unit, and no merge, else equal spans.  `list`: the keys in bf16 in the call's workspace, if it has room, and
+// the pipelined kernel's list there.  As in paged_cut() the host knows only the longest sequence, so these are estimates, in
+// microseconds, after 200 calls of 1 ... 128 sequences, each timed in all ways: the choice costs 1 % on the mean, 14 % at most.  Several
+// sequences of a unit each are taken to differ as the prompts of a trace do, six times as much being in the longest as in the mean:
+// in units a call takes the longest one's walk whatever the others hold.  (Spans / units / list: 4 of 540, 32 / 8 heads, 11.8 / 8.1, 64
+// of 510 20 / 11.5, 64 of 27 ... 8,400 34 / 77; 160 new tokens behind 1,000 38 / 17 / 51, 640 behind 10,000 174 / 132 / 142, 3 of up
+// to 640 behind up to 10,000 419 / - / 302; 24 x 5 drafted behind 10,000, 64 / 8 heads by heads 91 / 113.)
+// Chunks beside few-row sequences (`both`): whose the longest is, is not known, and units of 48 rows would have a single row's long walk
+// beside them.  (24 steps on up to 42,000 with 6 prompts of 1,100 127 us with a list, 252 without; on up to 6,000 with 6 x 250 behind
+// 4,000 161 and 97.)
+constexpr int64_t kMxMixedKeys = 8192;
 struct MxPlan {
     int nt, waves;
-    bool units;
+    bool units, list;
 };
-inline MxPlan mx_plan(int cu, int group, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
-    MxPlan p{1, 4, false};
+inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, bool both) {
+    MxPlan p{1, 4, false, false};
+    const int group = n_q_heads / n_kv_heads;
     const int64_t rows = len_q * group;
     auto cost = [&](int nt) { return (rows + 16 * nt - 1) / (16 * nt) * (10 + 3 * nt); };
     for (int nt = 2; nt <= 3; ++nt)
         if (cost(nt) < cost(p.nt)) p.nt = nt;
+    const bool alike = rows > 16 * p.nt || batch == 1;
     const double units = n_kv_heads * (rows <= 16 * p.nt ? (double)batch : (double)total_q * group / (16 * p.nt) + 0.5 * batch);
     if (units <= cu && p.nt == 1) p.waves = 8;
-    const double slots = cu * 8.0 / p.waves, tiles = len_k / 32.0;
-    const double step = (p.waves == 8 ? 1.0 : 0.72) * (1 + 0.35 * (p.nt - 1)), walk = step * std::ceil(tiles / p.waves);
-    const double as_units = 5.5 + std::max(walk, units / slots * walk);
-    const double as_spans = 11 + units * tiles * 0.19 * (1 + 0.5 * (p.nt - 1)) / cu / (batch == 1 ? 1 : 6);
-    p.units = as_units <= as_spans;
+    const double slots = cu * 8.0 / p.waves, longest = len_k / 32.0, mean = std::max(1.0, (len_k - 0.5 * len_q) / 32);
+    const double step = (p.nt == 3 ? 1.2 : p.nt == 2 ? 0.9 : p.waves == 8 ? 1.0 : 0.75) * (units > cu ? 1.35 : 1);
+    const double rounds = units / slots + (units > slots ? 0.5 : 0);
+    const double as_units = 6 + std::max(step * std::ceil(longest / p.waves), rounds * step * mean / p.waves);
+    const double ends = p.nt == 3 ? 25 + 0.1 * units : 13 + (p.nt == 2 ? 0.03 : 0.008) * units;
+    const double tiles = units * mean * (p.nt == 3 ? 0.23 : p.nt == 2 ? 0.2 : 0.19) / cu;
+    p.units = as_units <= ends + (alike ? tiles : tiles / 6);
+    const double as_list = paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, false) + 4 + (double)batch * len_k * n_kv_heads * 656 / 4.5e6;
+    p.list = rows > kPagedFewRows && (both ? len_k > kMxMixedKeys : as_list < std::min(as_units, ends + tiles));
     return p;
 }
 

@@ -73,7 +73,7 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
     using std::integral_constant;
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
     const int g = p.group;
-    const MxPlan plan = mx_plan(cu, g, p.n_kv_heads, batch, total_q, len_q, len_k);
+    const MxPlan plan = mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch, total_q, len_q, len_k, false);
     const int nt = plan.nt;
     const bool small = mx.log_page < 4;
     PagedMxStepParams s{};
@@ -227,11 +227,12 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const PagedLayout l = mx_layout(shape, batch->batch, batch->total_q, 0).paged;
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
-    // sequences with many rows: in the area, if it is there.  `both`: few-row sequences beside them, which stay with their codes;
-    // else all are taken there, and what finds no room, if that can be, is left to the steps as well.
-    const int64_t pages = l.capacity > 0 && len_q * g > kPagedFewRows ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
-    const bool list = pages > 0;
+    // Sequences with many rows: in the area, if it is there and that pays.  `both`: few-row sequences beside them, which stay with their
+    // codes; else all are taken there, and what finds no room, if that can be, is left to the steps as well.
     const bool both = batch->batch - (batch->total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2;
+    const int64_t pages = l.capacity > 0 && mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k, both).list
+                              ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
+    const bool list = pages > 0;
     const bool room = batch->batch * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
     const int few = g <= 16 ? 16 : g <= 32 ? 32 : 64;      // rows of such a sequence at most
     MxAreaParams a{};
