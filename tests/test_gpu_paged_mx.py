@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import mx_choice
 from paged_mx_reference import MxBatch, quantise, values
 from paged_reference import assert_attention, attention
 from paper_2409_15104_amd import binding as pec
@@ -167,13 +168,14 @@ def test_attention(seqs, hq, hkv, page, by_head, causal, flags):
 def test_attention_with_room_for_some_sequences(hq, hkv, page, hints, room):
     """Keys of sequences with many rows in bf16, as far as the workspace goes; all of them give the same."""
     seqs = [(1, 190), (70, 70), (150, 400), (1, 5), (0, 90), (40, 64), (1, 1), (300, 301), (1, 700)]
-    b = MxBatch(13, hq, hkv, page, seqs, spare_rows=2)
+    b = MxBatch(13, hq, hkv, page, seqs, spare_rows=2, table_extra=9000 // page)
     cache, table, cu, len_k = caches(b)
     ref = attention(b)
+    assert mx_choice.path(hq, hkv, seqs, (300, 9000) if hints else (0, 0), page, table.shape[1], 2, True) == "list"
     ws = torch.full((pec.pec_paged_mx_workspace_bytes(hq, hkv, len(seqs), b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
     out = torch.full((b.total, hq, 128), 55.0, dtype=torch.float32, device=DEV)
     lse = torch.full((hq, b.total), 55.0, device=DEV)
-    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=300 if hints else 0, max_len_k=700 if hints else 0,
+    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=300 if hints else 0, max_len_k=9000 if hints else 0,
                           out_dtype=torch.float32, out=out, lse=lse, workspace=ws)
     assert_attention(out, lse, ref)
     assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
