@@ -412,15 +412,11 @@ inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, 
 // in units a call takes the longest one's walk whatever the others hold.  (Spans / units / list: 4 of 540, 32 / 8 heads, 11.8 / 8.1, 64
 // of 510 20 / 11.5, 64 of 27 ... 8,400 34 / 77; 160 new tokens behind 1,000 38 / 17 / 51, 640 behind 10,000 174 / 132 / 142, 3 of up
 // to 640 behind up to 10,000 419 / - / 302; 24 x 5 drafted behind 10,000, 64 / 8 heads by heads 91 / 113.)
-// Chunks beside few-row sequences (`both`): whose the longest is, is not known, and units of 48 rows would have a single row's long walk
-// beside them.  (24 steps on up to 42,000 with 6 prompts of 1,100 127 us with a list, 252 without; on up to 6,000 with 6 x 250 behind
-// 4,000 161 and 97.)
-constexpr int64_t kMxMixedKeys = 8192;
 struct MxPlan {
     int nt, waves;
     bool units, list;
 };
-inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, bool both) {
+inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     MxPlan p{1, 4, false, false};
     const int group = n_q_heads / n_kv_heads;
     const int64_t rows = len_q * group;
@@ -438,7 +434,7 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
     const double tiles = units * mean * (p.nt == 3 ? 0.23 : p.nt == 2 ? 0.2 : 0.19) / cu;
     p.units = as_units <= ends + (alike ? tiles : tiles / 6);
     const double as_list = paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, false) + 4 + (double)batch * len_k * n_kv_heads * 656 / 4.5e6;
-    p.list = rows > kPagedFewRows && (both ? len_k > kMxMixedKeys : as_list < std::min(as_units, ends + tiles));
+    p.list = rows > kPagedFewRows && as_list < std::min(as_units, ends + tiles);
     return p;
 }
 

@@ -45,6 +45,7 @@ struct PagedBatch {
     // sequences (area_side 1) or for the others (0), which to the other launch are without queries
     const int32_t* area;
     int32_t area_side;
+    int32_t least_q, most_q;     // if most_q is not 0, the launch is for sequences with so many new tokens, and the others are without queries
 };
 
 struct PagedSeq {
@@ -56,6 +57,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& b, int i) {
     s.len_q = min(max(b.cu_q[i + 1], s.q0), b.total_q) - s.q0;
     s.len_k = min(max(b.len_k[i], 0), b.max_keys);
     if (b.area && (b.area[i] >= 0 ? 1 : 0) != b.area_side) s.len_q = 0;
+    if (b.most_q != 0 && (s.len_q < b.least_q || s.len_q > b.most_q)) s.len_q = 0;
     return s;
 }
 

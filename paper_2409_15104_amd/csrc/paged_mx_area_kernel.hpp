@@ -22,7 +22,6 @@ constexpr int kMxAreaHeadBytes = kMxAreaPage * kRowBytes;      // of a page
 struct MxAreaParams {
     PagedMx cache;
     PagedBatch batch;            // (area null: all sequences)
-    int32_t group, few_rows;     // sequences with at most so many rows per KV head stay with their codes
     int32_t capacity;            // pages
     int32_t n_kv_heads;
     int32_t* area;               // [batch] first page, -1: none
@@ -43,7 +42,7 @@ __global__ __launch_bounds__(1024) void paged_mx_area_kernel(const MxAreaParams 
         bool many = false;
         if (b < p.batch.batch) {
             const PagedSeq s = paged_seq(p.batch, b);
-            many = s.len_q * p.group > p.few_rows;
+            many = s.len_q > 0;
             pages = many ? (s.len_k + kMxAreaPage - 1) / kMxAreaPage : 0;
         }
         const int upto = wave_prefix(pages);      // (sums stop at 2^31 - 1, which is no page of any area)

@@ -67,13 +67,16 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
     return pages;
 }
 
-// The sequences of the call (of its side of the area) straight from their codes: spans and their merge.
-int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, char* ws,
+// The sequences of the launch straight from their codes: units, or spans and their merge.
+int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, bool beside, char* ws,
              hipStream_t st) {
     using std::integral_constant;
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
     const int g = p.group;
-    const MxPlan plan = mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch, total_q, len_q, len_k, false);
+    MxPlan plan = mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch, total_q, len_q, len_k);
+    // Chunks `beside` sequences with few rows, of which len_k may be: units, unless few chunks may have a very long walk.  (24 steps on
+    // up to 42,000 keys with 2 prompts of 250: the prompts as units 55 us, as spans 120.)
+    if (beside && (len_k <= 16384 || total_q * g / (16 * plan.nt) * p.n_kv_heads >= cu / 4)) plan.units = true;
     const int nt = plan.nt;
     const bool small = mx.log_page < 4;
     PagedMxStepParams s{};
@@ -227,21 +230,27 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const PagedLayout l = mx_layout(shape, batch->batch, batch->total_q, 0).paged;
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
-    // Sequences with many rows: in the area, if it is there and that pays.  `both`: few-row sequences beside them, which stay with their
-    // codes; else all are taken there, and what finds no room, if that can be, is left to the steps as well.
-    const bool both = batch->batch - (batch->total_q + len_q - 1) / std::max<int64_t>(1, len_q) > 2;
-    const int64_t pages = l.capacity > 0 && mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k, both).list
+    // Chunks beside sequences with few rows: each kind by itself, in units that suit it (24 steps on up to 42,000 keys with 6 prompts of
+    // 1,100: all in units of 48 rows 252 us, the prompts in the area, below, 127).
+    const int few_q = std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g);
+    if (len_q > few_q && batch->batch - (batch->total_q + len_q - 1) / len_q > 2) {
+        p.batch.least_q = 0;
+        p.batch.most_q = few_q;
+        if (int rc = mx_steps(p, mx, l, cu, few_q, len_k, false, ws, st)) return rc;
+        p.batch.least_q = few_q + 1;
+        p.batch.most_q = 0x7fffffff;
+        return mx_steps(p, mx, l, cu, len_q, len_k, true, ws, st);
+    }
+    // Chunks by themselves: in the area, if it is there and that pays; what finds no room, if that can be, is left to the steps.
+    const int64_t pages = l.capacity > 0 && mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k).list
                               ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
     const bool list = pages > 0;
     const bool room = batch->batch * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
-    const int few = g <= 16 ? 16 : g <= 32 ? 32 : 64;      // rows of such a sequence at most
     MxAreaParams a{};
     if (list) {
         const MxLayout m = mx_layout(shape, batch->batch, batch->total_q, pages);
         a.cache = mx;
         a.batch = p.batch;
-        a.group = g;
-        a.few_rows = both ? few : 0;
         a.capacity = (int32_t)pages;
         a.n_kv_heads = p.n_kv_heads;
         a.area = reinterpret_cast<int32_t*>(ws + m.off_area);
@@ -254,9 +263,9 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
         p.batch.area = a.area;
     }
-    if (!list || both || !room) {
+    if (!list || !room) {
         p.batch.area_side = 0;
-        if (int rc = mx_steps(p, mx, l, cu, list && both ? std::max<int64_t>(1, std::min<int64_t>(len_q, few / g)) : len_q, len_k, ws, st)) return rc;
+        if (int rc = mx_steps(p, mx, l, cu, len_q, len_k, false, ws, st)) return rc;
     }
     if (!list) return PEC_OK;
     const int64_t fill = std::min<int64_t>(pages * p.n_kv_heads, (int64_t)cu * 16);

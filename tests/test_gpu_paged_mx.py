@@ -162,22 +162,37 @@ def test_attention(seqs, hq, hkv, page, by_head, causal, flags):
         assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
 
 
-@pytest.mark.parametrize("room", [0, 100, 200, 100000])
 @pytest.mark.parametrize("hints", [True, False])
 @pytest.mark.parametrize("hq,hkv,page", [(8, 2, 16), (16, 16, 8), (6, 1, 128)])
-def test_attention_with_room_for_some_sequences(hq, hkv, page, hints, room):
-    """Keys of sequences with many rows in bf16, as far as the workspace goes; all of them give the same."""
-    seqs = [(1, 190), (70, 70), (150, 400), (1, 5), (0, 90), (40, 64), (1, 1), (300, 301), (1, 700)]
-    b = MxBatch(13, hq, hkv, page, seqs, spare_rows=2, table_extra=9000 // page)
+def test_chunks_beside_steps(hq, hkv, page, hints):
+    """Sequences with few rows and sequences with many are launched apart, each with their own cut."""
+    seqs = [(1, 190), (70, 70), (150, 400), (1, 5), (0, 90), (40, 64), (1, 1), (300, 301), (1, 700), (2, 30), (17, 17)]
+    b = MxBatch(13, hq, hkv, page, seqs, spare_rows=2, table_extra=20000 // page)
     cache, table, cu, len_k = caches(b)
     ref = attention(b)
-    assert mx_choice.path(hq, hkv, seqs, (300, 9000) if hints else (0, 0), page, table.shape[1], 2, True) == "list"
-    ws = torch.full((pec.pec_paged_mx_workspace_bytes(hq, hkv, len(seqs), b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
+    assert mx_choice.path(hq, hkv, seqs, (300, 700) if hints else (0, 0), page, table.shape[1], 2, True) == "beside"
+    ws = torch.full((pec.pec_paged_mx_workspace_bytes(hq, hkv, len(seqs), b.total),), 0xff, dtype=torch.uint8, device=DEV)
     out = torch.full((b.total, hq, 128), 55.0, dtype=torch.float32, device=DEV)
     lse = torch.full((hq, b.total), 55.0, device=DEV)
-    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=300 if hints else 0, max_len_k=9000 if hints else 0,
+    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=300 if hints else 0, max_len_k=700 if hints else 0,
                           out_dtype=torch.float32, out=out, lse=lse, workspace=ws)
     assert_attention(out, lse, ref)
+    assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
+
+
+@pytest.mark.parametrize("room", [0, 520, 1400, 3000, 100000])
+def test_chunks_with_room_for_some(room):
+    """Keys of sequences in bf16 as far as the workspace goes; all of them give the same."""
+    seqs = [(500, 500), (400, 900), (300, 300)]
+    b = MxBatch(13, 32, 8, 64, seqs, spare_rows=2, table_extra=600)
+    cache, table, cu, len_k = caches(b)
+    assert mx_choice.path(32, 8, seqs, (512, 30512), 64, table.shape[1], 2, True) == "list"
+    ws = torch.full((pec.pec_paged_mx_workspace_bytes(32, 8, len(seqs), b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
+    out = torch.full((b.total, 32, 128), 55.0, dtype=torch.float32, device=DEV)
+    lse = torch.full((32, b.total), 55.0, device=DEV)
+    pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, max_len_q=512, max_len_k=30512, out_dtype=torch.float32, out=out, lse=lse,
+                          workspace=ws)
+    assert_attention(out, lse, attention(b))
     assert bool((out[b.rows:] == 55).all()) and bool((lse[:, b.rows:] == 55).all())
 
 

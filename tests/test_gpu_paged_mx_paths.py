@@ -42,7 +42,8 @@ CASES = [      # heads, KV heads, page, by head, sequences, hints, room, path
     (32, 8, 64, False, [(512, 700)], (512, 30512), 700, "list"),
     (32, 8, 64, True, [(512, 700)], (512, 30512), 40000, "list"),        # room for all that the table could hold
     (32, 8, 64, False, [(512, 700)], (512, 30512), 300, "list"),         # no room: the steps take it
-    (8, 2, 16, False, [(1, 300)] * 4 + [(150, 150), (90, 700)], (150, 9000), 5000, "list"),
+    (8, 2, 16, False, [(1, 300)] * 4 + [(150, 150), (90, 700)], (150, 9000), 0, "beside"),
+    (8, 2, 16, True, [(1, 300)] * 6 + [(150, 20000)], (150, 20000), 0, "beside"),
 ]
 
 

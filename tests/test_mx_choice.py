@@ -16,9 +16,13 @@ def test_long_chunks_go_to_the_list_where_it_pays():
     assert path(32, 8, [(512, 30512)], (512, 30512), 64, 477, room=True) == "list"
     assert path(32, 8, [(512, 30512)], (512, 30512), 64, 477) == "spans 3"
     assert path(32, 8, [(640, 1640)], (640, 1640), 16, 103, room=True) == "units 3 4"
+
+
+def test_chunks_beside_steps_are_launched_apart():
     mixed = [(1, 3500)] * 24 + [(1100, 1100)] * 6
-    assert path(32, 8, mixed, (1100, 42000), 16, 2625, room=True) == "list"
-    assert path(32, 8, mixed, (1100, 3500), 16, 219, room=True) != "list"
+    assert path(32, 8, mixed, (1100, 42000), 16, 2625, room=True) == "beside"
+    assert path(32, 8, mixed, (0, 0), 16, 219) == "beside"
+    assert path(32, 8, [(5, 3500)] * 24, (5, 3500), 16, 219) != "beside"
 
 
 def test_unknown_hints_are_taken_from_the_table():
