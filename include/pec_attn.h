@@ -450,11 +450,14 @@ int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
 /*
  * pec_attn_paged over a paged cache in 4 bits: the same arguments, masks, empty rows, hidden values, hints and limits; keys and
  * values are what the codes stand for, exactly.
- *   workspace: pec_paged_mx_workspace_bytes(shape, batch, total_q, total_k) bytes, 16-byte aligned.  total_k is a number of keys that room
- *              is made for (512 bytes per key and KV head): sequences with many new tokens have their keys turned into bf16 there, once
- *              for all of their rows, which is what makes them as fast as on a cache of bf16; those that find no room, and all of
- *              them with total_k = 0, are worked on straight from the codes, which gives the same results but for rounding and
- *              takes longer.  Any workspace of at least the size for total_k = 0 will do.
+ *   workspace: pec_paged_mx_workspace_bytes(shape, batch, total_q, total_k) bytes, 16-byte aligned, whatever they hold; calls that may
+ *              run at the same time need one each.  total_k is a number of keys that room is made for (512 bytes per key and KV head):
+ *              in calls with nothing but chunks, sequences that find room have their keys turned into bf16 there, once for all of their
+ *              rows, where that is faster; those that find none, and all of them with total_k = 0, are worked on straight from the
+ *              codes, which gives the same results but for rounding.  Any workspace of at least the size for total_k = 0 will do.
+ *              (512 new tokens behind 28,400, 32 / 8 heads: 260 us with room, 360 without.)
+ * A cache laid out by heads ([pages, heads, slots, 64]) is read up to a fifth faster than one by token: 64 bytes are half a cache line.
+ * Against 64 bits, on what the codes stand for, a bf16 result is off by 2.0e-3 ... 2.4e-3 of its 2-norm.
  */
 int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cache, const pec_paged_batch_t* batch, const void* q,
                       int64_t q_stride, int causal, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
