@@ -455,7 +455,7 @@ int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
  *              in calls with nothing but chunks, sequences that find room have their keys turned into bf16 there, once for all of their
  *              rows, where that is faster; those that find none, and all of them with total_k = 0, are worked on straight from the
  *              codes, which gives the same results but for rounding.  Any workspace of at least the size for total_k = 0 will do.
- *              (512 new tokens behind 28,400, 32 / 8 heads: 260 us with room, 360 without.)
+ *              (512 new tokens behind 28,400, 32 / 8 heads: 260 us with room, 400 without.)
  * A cache laid out by heads ([pages, heads, slots, 64]) is read up to a fifth faster than one by token: 64 bytes are half a cache line.
  * Against 64 bits, on what the codes stand for, a bf16 result is off by 2.0e-3 ... 2.4e-3 of its 2-norm.
  */

@@ -4,7 +4,7 @@
 // A chunk's rows read every key many times (512 tokens of 4 heads to a KV head: eight workgroups of 256 rows), the conversion would be
 // done as often, and the tile loop of fwd_il_kernel has neither a register nor an issue slot to spare for it.  Done once it is
 // 136 bytes in and 512 out per key and KV head, memory-bound: 28,900 keys of 8 heads (156 MB) 34 us, 4.6 TB/s; the pages are dealt out
-// in 4 us.  512 new tokens on them, 32 / 8 heads, take 260 us in all, straight from the codes 360.
+// in 4 us.  512 new tokens on them, 32 / 8 heads, take 260 us in all, straight from the codes 400.
 //
 // The area is a paged cache of its own, pages of 64 keys by heads; a sequence has consecutive pages, so its row of the block table is
 // a stretch of one table that counts 0, 1, 2 ..., beginning at the sequence's first page.
