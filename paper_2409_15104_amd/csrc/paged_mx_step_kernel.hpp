@@ -132,23 +132,34 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
         if (len <= 0) return;
     }
 
+    // The call's arguments, loaded where they are used: what only a piece's start and end want is not kept in scalar registers.
+    auto arguments = []() {
+        typedef const __attribute__((address_space(4))) PagedMxStepParams* Kernarg;
+        Kernarg at = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(at));
+        PagedMxStepParams q;
+        __builtin_memcpy(&q, (const PagedMxStepParams*)at, sizeof(q));
+        return q;
+    };
+
     // Row tile `rt` of sequence `seq`; uniform.  (The sequence itself is looked up where it is needed: scalar registers are short.)
     struct Unit {
         int seq, rt, keys, tiles;
     };
-    auto unit_of = [&](const PagedSeq& s, int seq, int rt) {
+    auto unit_of = [&](const MxCut& cut, const PagedSeq& s, int seq, int rt) {
         const int keys = cut.keys(s, rt);
         return Unit{seq, rt, keys, max(1, (keys + kStepTile - 1) / kStepTile)};
     };
     auto next_unit = [&](const Unit& u) {
+        const PagedMxStepParams p = arguments();
         int seq = u.seq, rt = u.rt + 1;
-        PagedSeq s = line.seq(seq);
-        while (rt >= cut.row_tiles(s)) {
+        PagedSeq s = line.seq(seq, p.a.batch);
+        while (rt >= p.cut.row_tiles(s)) {
             rt = 0;
-            if (++seq >= bt.batch) return Unit{0, 0, 0, 1};       // (never, unless the offsets change under the launch)
-            s = line.seq(seq);
+            if (++seq >= p.a.batch.batch) return Unit{0, 0, 0, 1};       // (never, unless the offsets change under the launch)
+            s = line.seq(seq, p.a.batch);
         }
-        return unit_of(s, seq, rt);
+        return unit_of(p.cut, s, seq, rt);
     };
     Unit unit;
     int tile;
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
             }
         }
         if (rt < 0 || rt >= n_rt) return;    // (never, as above)
-        unit = unit_of(s, seq, rt);
+        unit = unit_of(cut, s, seq, rt);
         tile = UNITS ? 0 : at;
         if constexpr (UNITS) len = unit.tiles;
     }
@@ -260,16 +271,17 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
     f32x4 o[NT][8];
     float m_run[NT], l_run[NT];    // softmax reference (kNoKey: no key yet; finite, so that it can be subtracted), denominators
     auto begin_piece = [&]() {
+        const PagedMxStepParams p = arguments();
         const int last = unit.keys - 1, row0 = unit.rt * R;
-        const PagedSeq seq = line.seq(unit.seq);
+        const PagedSeq seq = line.seq(unit.seq, p.a.batch);
         q0 = seq.q0;
-        rows = min(R, seq.len_q * g - row0);
+        rows = min(R, seq.len_q * p.a.group - row0);
         end = min(unit.tiles, tile + len - done);
-        first_vis = causal ? seq.len_k - seq.len_q + cut.group.div(row0) : last;       // last key of the first row
+        first_vis = p.cut.causal ? seq.len_k - seq.len_q + p.cut.group.div(row0) : last;       // last key of the first row
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = row0 + nt * 16 + m, pos = cut.group.div(row), head = kvh * g + row - pos * g;
-            last_vis[nt] = causal ? min(last, seq.len_k - seq.len_q + pos) : last;
+            const int row = row0 + nt * 16 + m, pos = p.cut.group.div(row), head = kvh * p.a.group + row - pos * p.a.group;
+            last_vis[nt] = p.cut.causal ? min(last, seq.len_k - seq.len_q + pos) : last;
             // rows without a query stay zero and are not stored
             const __bf16* qrow = p.a.q + (q0 + pos) * p.a.q_stride + (int64_t)head * kHeadDim + 32 * c;
 #pragma unroll
@@ -471,6 +483,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
     // a row leaves as one run) touch all banks evenly.
     float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
     auto finish_piece = [&](int piece0) {
+        const PagedMxStepParams p = arguments();
         const bool whole = piece0 == 0 && end == unit.tiles;
         const int row0 = unit.rt * R;
         const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
@@ -481,10 +494,10 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
             if (nt * 16 >= rows) break;
             const float l_tot = across(l_run[nt], [](float a, float b) { return a + b; });
             if constexpr (WAVES == 1) {      // nobody to join
-                const int flat = row0 + nt * 16 + m, pos = cut.group.div(flat), head = kvh * g + flat - pos * g, token = q0 + pos;
+                const int flat = row0 + nt * 16 + m, pos = p.cut.group.div(flat), head = kvh * p.a.group + flat - pos * p.a.group, token = q0 + pos;
                 if (nt * 16 + m >= rows) continue;
                 const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-                float* const to = whole ? p.a.lse + (int64_t)head * bt.total_q + token : p.part_lse + slot_row + nt * 16 + m;
+                float* const to = whole ? p.a.lse + (int64_t)head * p.a.batch.total_q + token : p.part_lse + slot_row + nt * 16 + m;
                 if (c == 0) *to = l_tot == 0.f ? -INFINITY : (m_run[nt] + __builtin_amdgcn_logf(l_tot)) * kLn2;      // NaN from NaN weights
                 const int64_t row = whole ? (int64_t)token * p.a.n_q_heads + head : slot_row + nt * 16 + m;
 #pragma unroll
@@ -521,8 +534,8 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
                 const float inv = den == 0.f ? 0.f : 1.f / den;
                 join_w[k * 16 + row] = __builtin_amdgcn_exp2f(join_m[k * 16 + row] - mx) * inv;
                 if (k == 0 && nt * 16 + row < rows) {
-                    const int flat = row0 + nt * 16 + row, pos = cut.group.div(flat);
-                    float* const to = whole ? p.a.lse + (int64_t)(kvh * g + flat - pos * g) * bt.total_q + q0 + pos : p.part_lse + slot_row + nt * 16 + row;
+                    const int flat = row0 + nt * 16 + row, pos = p.cut.group.div(flat);
+                    float* const to = whole ? p.a.lse + (int64_t)(kvh * p.a.group + flat - pos * p.a.group) * p.a.batch.total_q + q0 + pos : p.part_lse + slot_row + nt * 16 + row;
                     *to = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * kLn2;      // NaN from NaN weights
                 }
             }
@@ -530,7 +543,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
             const int ch = tid & 31;
 #pragma unroll
             for (int pass = 0; pass < 8 / WAVES; ++pass) {
-                const int row = pass * 2 * WAVES + (tid >> 5), flat = row0 + nt * 16 + row, pos = cut.group.div(flat);
+                const int row = pass * 2 * WAVES + (tid >> 5), flat = row0 + nt * 16 + row, pos = p.cut.group.div(flat);
                 f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < WAVES; ++k) {
@@ -540,7 +553,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
                     for (int i = 0; i < 4; ++i) z[i] = fmaf(wgt, y[i], z[i]);
                 }
                 if (nt * 16 + row < rows) {
-                    const int64_t to = whole ? (int64_t)(q0 + pos) * p.a.n_q_heads + kvh * g + flat - pos * g : slot_row + nt * 16 + row;
+                    const int64_t to = whole ? (int64_t)(q0 + pos) * p.a.n_q_heads + kvh * p.a.group + flat - pos * p.a.group : slot_row + nt * 16 + row;
                     if (f32) *reinterpret_cast<f32x4*>(dst + to * kHeadDim + 4 * ch) = z;
                     else *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.a.out) + to * kHeadDim + 4 * ch) = __builtin_convertvector(z, bf16x4);
                 }

@@ -142,7 +142,8 @@ struct PagedLine {
         for (int c = lane; c < n_chunks; c += 64) sum = add_up(sum, chunk_sum[c]);
         total = __builtin_amdgcn_readlane(wave_prefix(sum), 63);
     }
-    __device__ __forceinline__ PagedSeq seq(int i) const {       // uniform
+    __device__ __forceinline__ PagedSeq seq(int i) const { return seq(i, bt); }
+    __device__ __forceinline__ PagedSeq seq(int i, const PagedBatch& bt) const {       // uniform; bt: the same batch
         PagedSeq s;
         if (n_chunks <= 1) {
             s.q0 = __builtin_amdgcn_readlane(lanes.q0, i);
