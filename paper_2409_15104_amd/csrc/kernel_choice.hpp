@@ -411,7 +411,7 @@ inline PagedCut paged_cut(int cu, int n_q_heads, int n_kv_heads, int64_t batch, 
 // sequences of a unit each are taken to differ as the prompts of a trace do, six times as much being in the longest as in the mean:
 // in units a call takes the longest one's walk whatever the others hold.  (Spans / units / list: 4 of 540, 32 / 8 heads, 11.8 / 8.1, 64
 // of 510 20 / 11.5, 64 of 27 ... 8,400 34 / 77; 160 new tokens behind 1,000 38 / 17 / 51, 640 behind 10,000 174 / 132 / 142, 3 of up
-// to 640 behind up to 10,000 419 / - / 302; 24 x 5 drafted behind 10,000, 64 / 8 heads by heads 91 / 113.)
+// to 640 behind up to 10,000 419 / - / 302; 24 x 5 drafted behind 10,000, 64 / 8 heads by heads 83 / 113.)
 struct MxPlan {
     int nt, waves;
     bool units, list;

@@ -21,7 +21,7 @@
 //
 // What bounds it: by heads memory, 4 sequences of 107,500 tokens, 64 / 8 heads (488 MB) 85 us with the merge, 120 of 3,300, 32 / 8 (435
 // MB) 90, 5.0 TB/s while the spans run, where the loads alone take 82; by token half cache lines, 105 us for the former.  24 x 5 drafted tokens on
-// 10,350, 64 / 8 heads, 48 rows: instructions, 260 of the vector ALU and 48 matrix products for a tile, 91 us by heads.  640 new
+// 10,350, 64 / 8 heads, 48 rows: instructions, 270 of the vector ALU and 48 matrix products for a tile, 83 us by heads, 89 by token.  640 new
 // tokens behind 1,000, 32 / 8, in units: 27 us.  4 of 540 in units: 8 us, latency.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -132,7 +132,8 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
         if (len <= 0) return;
     }
 
-    // The call's arguments, loaded where they are used: what only a piece's start and end want is not kept in scalar registers.
+    // The call's arguments, loaded where they are used: what only a piece's start and end want is not kept in scalar registers, of which
+    // 60 ... 98 were spilled to vector registers, and vector registers to memory (24 x 5 drafted tokens 110 us, now 89).
     auto arguments = []() {
         typedef const __attribute__((address_space(4))) PagedMxStepParams* Kernarg;
         Kernarg at = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();

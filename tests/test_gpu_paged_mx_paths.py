@@ -228,3 +228,54 @@ def test_rounding_on_the_way_in_is_what_attention_reads():
     assert_attention(out, lse, attention(b))
     c, s = quantise(b.raw[0][0])
     assert torch.equal(values(c, s), b.keys[0])
+
+
+@pytest.mark.parametrize("flags", [0, pec.PEC_FLAG_SIMPLE_KERNEL])
+@pytest.mark.parametrize("page", [8, 16])
+def test_tables_without_a_page(page, flags):
+    """No page for any token: nothing is stored, rows come back as zeros, every row is empty."""
+    z = lambda *s: torch.full(s, 255, dtype=torch.uint8, device=DEV)  # noqa: E731
+    cache = pec.PagedCacheMx(z(2, page, 2, 64), z(2, page, 2, 64), z(2, 2, 4, page), z(2, 2, 4, page))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    table, cu, len_k = torch.empty(2, 0, dtype=torch.int32, device=DEV), i32(0, 3, 5), i32(0, 90)
+    q, k = torch.ones(6, 4, 128, dtype=torch.bfloat16, device=DEV), torch.ones(6, 2, 128, dtype=torch.bfloat16, device=DEV)
+    pec.pec_paged_append_mx(k, k, cache, table, cu, len_k)
+    assert bool((cache.k == 255).all()) and bool((cache.v_scale == 255).all())
+    back = pec.pec_paged_read_mx(cache, table, cu, len_k, k=k.clone(), v=k.clone())
+    for t in back:
+        assert bool((t[:5] == 0).all()) and bool((t[5:] == 1).all())
+    for causal in (True, False):
+        out, lse = torch.ones_like(q), torch.ones(4, 6, device=DEV)
+        pec.pec_attn_paged_mx(q, cache, table, cu, len_k, causal=causal, flags=flags, out=out, lse=lse)
+        assert bool((out[:5] == 0).all()) and bool((lse[:, :5] == -math.inf).all())
+        assert bool((out[5:] == 1).all()) and bool((lse[:, 5:] == 1).all())
+
+
+def test_offsets_that_fall_stay_in_bounds():
+    """Malformed offsets and lengths: whatever comes out, nothing behind the last packed row or outside the results is touched."""
+    b = MxBatch(31, 8, 2, 16, [(1, 90), (40, 70), (3, 33), (1, 5), (20, 20)], spare_rows=3)
+    held, table, _, _ = b.to(DEV)
+    cache, q = pec.PagedCacheMx(*held), b.q.to(DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    for cu, len_k in ((i32(0, 50, 3, 60, 10, 68), i32(90, 70, 33, 5, 20)), (i32(-5, 2 ** 30, -7, 0, 2 ** 31 - 1, 1), i32(-4, 2 ** 31 - 1, 0, 10 ** 6, 64))):
+        for room in (0, 500):
+            guard = torch.full((b.total + 8, 8, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+            lguard = torch.full((8 * b.total + 64,), 9.0, device=DEV)
+            out, lse = guard[:b.total], lguard[:8 * b.total].view(8, b.total)
+            pec.pec_attn_paged_mx(q, cache, table, cu, len_k, out=out, lse=lse, total_k=room)
+            torch.cuda.synchronize()
+            assert bool((guard[b.total:] == 9).all()) and bool((lguard[8 * b.total:] == 9).all())
+
+
+def test_results_do_not_depend_on_what_ran_before():
+    """The same call twice, with other calls on the same workspace between: equal to the last bit."""
+    b = MxBatch(32, 16, 8, 16, [(1, 6000), (1, 40), (6, 900), (6, 6)])
+    held, table, cu, len_k = b.to(DEV)
+    cache, q = pec.PagedCacheMx(*held), b.q.to(DEV)
+    ws = torch.empty(pec.pec_paged_mx_workspace_bytes(16, 8, 4, b.total, 3000), dtype=torch.uint8, device=DEV)
+    call = lambda **kw: pec.pec_attn_paged_mx(q, cache, table, cu, len_k, out_dtype=torch.float32, workspace=ws, **kw)  # noqa: E731
+    first = call(max_len_q=6, max_len_k=6000)
+    for other in (dict(max_len_q=1, max_len_k=40), dict(), dict(max_len_q=14, max_len_k=9000)):
+        call(**other)
+        again = call(max_len_q=6, max_len_k=6000)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
