@@ -448,8 +448,8 @@ int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
                       void* v_out, void* stream);
 
 /*
- * pec_attn_paged over a paged cache in 4 bits: the same arguments, masks, empty rows, hidden values, hints and limits; keys and
- * values are what the codes stand for, exactly.
+ * pec_attn_paged over a paged cache in 4 bits: the same arguments, masks, empty rows, hidden values and hints; keys and values are what
+ * the codes stand for, exactly.  The same limits, steps of 32 keys being counted for blocks of 16 rows.
  *   workspace: pec_paged_mx_workspace_bytes(shape, batch, total_q, total_k) bytes, 16-byte aligned, whatever they hold; calls that may
  *              run at the same time need one each.  total_k is a number of keys that room is made for (512 bytes per key and KV head):
  *              in calls with nothing but chunks, sequences that find room have their keys turned into bf16 there, once for all of their

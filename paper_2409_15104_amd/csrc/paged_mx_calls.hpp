@@ -78,6 +78,9 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
     // up to 42,000 keys with 2 prompts of 250: the prompts as units 55 us, as spans 120.)
     if (beside && (len_k <= 16384 || total_q * g / (16 * plan.nt) * p.n_kv_heads >= cu / 4)) plan.units = true;
     const int nt = plan.nt;
+    // units of a KV head at most: of all packed rows, or of sequences that this launch is for
+    int64_t row_tiles = total_q * g / (16 * nt) + batch;
+    if (p.batch.most_q != 0) row_tiles = std::min(row_tiles, batch * (((int64_t)p.batch.most_q * g + 16 * nt - 1) / (16 * nt)));
     const bool small = mx.log_page < 4;
     PagedMxStepParams s{};
     s.a = p;
@@ -100,7 +103,7 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
         // two heads to a workgroup where they share cache lines (64 sequences of 510: 17.6 us with one, 11.7 with two)
         const int heads = nt == 1 && plan.waves == 4 && mx_by_token(mx) && p.n_kv_heads % 2 == 0 ? 2 : 1;
         s.kv_heads = fast_div(p.n_kv_heads / heads);
-        const int64_t groups = (total_q * g / (16 * nt) + batch) * s.kv_heads.d;
+        const int64_t groups = row_tiles * s.kv_heads.d;
         if (groups > 0x7fffff00) return PEC_ERR_UNSUPPORTED;
         grid = dim3((unsigned)std::min<int64_t>((groups + 7) / 8 * 8, kUnitsRow), (unsigned)((groups + kUnitsRow - 1) / kUnitsRow));
         if (nt == 3) launch(three, four, one, yes, no);
@@ -122,7 +125,6 @@ int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, 
     s.n_spans = fast_div(groups / lines);
     s.kv_heads = fast_div(lines);
     s.unit_rows = (int32_t)std::min<int64_t>(16 * nt, len_q * g);
-    const int64_t row_tiles = total_q * g / (16 * nt) + batch;
     if ((double)row_tiles * (p.batch.max_keys / kStepTile + 1) > 2147483647.0) return PEC_ERR_UNSUPPORTED;      // every tile step has a number
     grid = dim3((unsigned)groups);
     if (side_by_side) launch(one, one, eight, no, no);
