@@ -205,3 +205,24 @@ def test_one_chunk(causal, room):
     ws = torch.full((pec.pec_paged_mx_workspace_bytes(8, 2, 1, b.total, room),), 0xff, dtype=torch.uint8, device=DEV)
     out, lse = pec.pec_attn_paged_mx(b.q.to(DEV), cache, table, cu, len_k, causal=causal, workspace=ws)
     assert_attention(out, lse, attention(b, causal))
+
+
+def test_two_tokens_for_one_slot():
+    """Sequences that share a page: its slots hold bytes of one or the other, and nothing else changes."""
+    hkv = 2
+    b = MxBatch(6, 4, hkv, 16, [(3, 19), (3, 19), (2, 8)])
+    b.table[1, 1] = b.table[0, 1]                # positions 16, 17, 18 of both
+    pages, slots, k, v = rows_of(b)
+    cache, table, cu, len_k = caches(b)
+    pec.pec_paged_append_mx(k.to(DEV), v.to(DEV), cache, table, cu, len_k)
+    for got_c, got_s, c, s, x in ((cache.k, cache.k_scale, b.k, b.k_scale, k), (cache.v, cache.v_scale, b.v, b.v_scale, v)):
+        got_c, got_s, (codes, scales) = got_c.cpu(), got_s.cpu(), quantise(x)
+        for i in range(3):
+            at = (pages[i], slots[i])
+            assert bool(((got_c[at] == codes[i]) | (got_c[at] == codes[3 + i])).all())
+            mine = got_s[at[0], :, :, at[1]]
+            assert bool(((mine == scales[i]) | (mine == scales[3 + i])).all())
+        want_c, want_s = c.clone(), s.clone()
+        want_c[pages, slots], want_s[pages, :, :, slots] = codes, scales
+        want_c[pages[:3], slots[:3]], want_s[pages[:3], :, :, slots[:3]] = got_c[pages[:3], slots[:3]], got_s[pages[:3], :, :, slots[:3]]
+        assert torch.equal(got_c, want_c) and torch.equal(got_s, want_s)
