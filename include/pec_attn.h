@@ -387,7 +387,8 @@ int pec_paged_append(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope,
  * cached prefix and whole prompts may be mixed.
  *   q [total_q, Hq, 128] with q_stride elements from token to token (0 = packed); out [total_q, Hq, 128] in shape->out_dtype,
  *   lse [Hq, total_q].  Rows without a visible key get out = 0, lse = -inf; a row whose weights are NaN gets NaN in both; an
- *   infinite value that a row sees gives that infinity (NaN with one of the other sign).
+ *   infinite value that a row sees gives that infinity (NaN with one of the other sign; either of them where its score is some 87 or
+ *   more below the row's largest, so that its weight is 0 in fp32).
  *   Weights are rounded to bf16 once, for their product with the values (PEC_FLAG_SIMPLE_KERNEL: not at all); scores, sums,
  *   partial results and their merge are fp32.  Against 64 bits a bf16 result is off by 2.0e-3 ... 2.4e-3 of its 2-norm, with
  *   weights in fp32 by 1.6e-3 ... 1.7e-3, of which its own rounding is most.

@@ -443,6 +443,11 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
                         if (b >> 16 * i & 0xffff) odd_keys |= 1u << (16 * (e >> 2) + 4 * i + (e & 3));
                 }
                 odd_keys = __builtin_amdgcn_readfirstlane(odd_keys);
+                // (an infinity or NaN goes in with the weight 1, as its own may be 0 in fp32)
+                auto added = [](float to, float weight, uint32_t y) {
+                    const float value = __builtin_bit_cast(float, y);
+                    return fmaf((y & 0x7f800000u) == 0x7f800000u ? 1.f : weight, value, to);
+                };
                 // (a key's 16 bytes for the dims of this lane's results are read again: few registers, and seldom)
                 const ConstInts table = (ConstInts)(uintptr_t)(bt.table + (int64_t)unit.seq * bt.table_len);
 #pragma unroll 1
@@ -461,11 +466,12 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
                         if (at_key > last_vis[x]) continue;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
+                            __builtin_amdgcn_sched_barrier(0);
                             const u32x4 y = mx_values(codes[i], scale);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                o[x][2 * j][i] = fmaf(weight, __builtin_bit_cast(float, y[j] << 16), o[x][2 * j][i]);
-                                o[x][2 * j + 1][i] = fmaf(weight, __builtin_bit_cast(float, y[j] & 0xffff0000u), o[x][2 * j + 1][i]);
+                                o[x][2 * j][i] = added(o[x][2 * j][i], weight, y[j] << 16);
+                                o[x][2 * j + 1][i] = added(o[x][2 * j + 1][i], weight, y[j] & 0xffff0000u);
                             }
                         }
                     }
@@ -485,6 +491,9 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
     float *const join_m = joint, *const join_l = joint + WAVES * 16, *const join_w = joint + 2 * WAVES * 16;
     auto finish_piece = [&](int piece0) {
         const PagedMxStepParams p = arguments();
+        int lane = threadIdx.x & 63, tid = threadIdx.x % (WAVES * 64);
+        asm volatile("" : "+v"(lane), "+v"(tid));      // places in LDS and in the results are worked out here, too
+        const int m = lane & 15, c = lane >> 4;
         const bool whole = piece0 == 0 && end == unit.tiles;
         const int row0 = unit.rt * R;
         const int64_t slot_row = (int64_t)(2 * w + (piece0 == 0 ? 1 : 0)) * R;      // of n_spans x KV heads x 2
