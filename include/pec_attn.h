@@ -454,10 +454,14 @@ int pec_paged_read_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
  * the codes stand for, exactly.  The same limits, steps of 32 keys being counted for blocks of 16 rows.
  *   workspace: pec_paged_mx_workspace_bytes(shape, batch, total_q, total_k) bytes, 16-byte aligned, whatever they hold; calls that may
  *              run at the same time need one each.  total_k is a number of keys that room is made for (512 bytes per key and KV head):
- *              in calls with nothing but chunks, sequences that find room have their keys turned into bf16 there, once for all of their
- *              rows, where that is faster; those that find none, and all of them with total_k = 0, are worked on straight from the
- *              codes, which gives the same results but for rounding.  Any workspace of at least the size for total_k = 0 will do.
- *              (512 new tokens behind 28,400, 32 / 8 heads: 260 us with room, 400 without.)
+ *              sequences with many new tokens that find room, in their order, have their keys turned into bf16 there, once for all of
+ *              their rows, where the estimates say that this is faster, decode steps beside them or not; those that find none, and all
+ *              of them with total_k = 0, are worked on straight from the codes, which gives the same results but for rounding.  The sum
+ *              of such sequences' seqlens_k is enough, and tells the estimates more than a larger one.  Any workspace of at least the
+ *              size for total_k = 0 will do.  (512 new tokens behind 28,400, 32 / 8 heads: 260 us with room, 400 without; 512 behind
+ *              30,000 beside 24 decode steps 298 and 405, 8,192 behind 54,000 beside them 5,910 and 8,110.)
+ * Without max_len_q decode steps cannot be told from a prompt: a launch that finds nothing to do is added to theirs (64 of 540 tokens
+ * 14 us, with hints 11).
  * A cache laid out by heads ([pages, heads, slots, 64]) is read up to a fifth faster than one by token: 64 bytes are half a cache line.
  * Against 64 bits, on what the codes stand for, a bf16 result is off by 2.0e-3 ... 2.4e-3 of its 2-norm.
  */

@@ -416,7 +416,11 @@ struct MxPlan {
     int nt, waves;
     bool units, list;
 };
-inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+struct MxCost {
+    MxPlan plan;
+    double units, spans, list;
+};
+inline MxCost mx_cost(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
     MxPlan p{1, 4, false, false};
     const int group = n_q_heads / n_kv_heads;
     const int64_t rows = len_q * group;
@@ -435,7 +439,46 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
     p.units = as_units <= ends + (alike ? tiles : tiles / 6);
     const double as_list = paged_list_us(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k, false) + 4 + (double)batch * len_k * n_kv_heads * 656 / 4.5e6;
     p.list = rows > kPagedFewRows && as_list < std::min(as_units, ends + tiles);
-    return p;
+    return MxCost{p, as_units, ends + tiles, as_list};
+}
+inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k) {
+    return mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k).plan;
+}
+
+// A call on a cache in 4 bits as a whole.  `apart`: sequences with few rows, up to few_q new tokens, and those with many are launched
+// by themselves, each in units that suit them; `many` is the plan of the latter (of all sequences, if nothing is apart).  Its `list`:
+// their keys go to the area, `pages` pages of 64 keys that the workspace has room for, as far as they find it there.
+//
+// The longest have to leave room for more than two with few rows.  Of the sequences
+// with many rows the host knows the longest one's tokens and how many tokens there are: they are taken to be all that long, every
+// other sequence having one token.  Whether the longest one's keys are theirs it does not know, so the estimates without a prefix
+// and with one count alike, the latter with as many keys among them as one sequence can have, or as the area has room for: a
+// workspace made for prompts that begin here (total_k) says that no long prefix is behind them.
+//
+// (512 tokens behind 30,000 beside 24 steps on 3,500, 32 / 8 heads, with room 298 us, straight from the codes 405; 8,192 behind 54,000
+// 5,910 / 8,110; 128 behind 40,000 180 in spans, 349 in units.)
+struct MxCall {
+    int few_q;
+    bool apart;
+    MxPlan many;
+};
+inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, int64_t pages) {
+    const int g = n_q_heads / n_kv_heads;
+    MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, mx_plan(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k)};
+    if (len_q > c.few_q && batch - (total_q + len_q - 1) / len_q > 2) {
+        const int64_t n = std::min(batch, std::max<int64_t>(1, (total_q - batch + (len_q - 1) / 2) / (len_q - 1)));
+        const int64_t tokens = std::max(len_q, total_q - (batch - n));
+        const int64_t prefix = std::max(len_q, pages > 0 ? std::min(len_k, 64 * pages / n) : len_k / n);
+        const MxCost with = mx_cost(cu, n_q_heads, n_kv_heads, n, tokens, len_q, prefix);
+        const MxCost none = mx_cost(cu, n_q_heads, n_kv_heads, n, tokens, len_q, len_q);
+        MxCost mean{with.plan, (with.units + none.units) / 2, (with.spans + none.spans) / 2, (with.list + none.list) / 2};
+        mean.plan.units = mean.units <= mean.spans;
+        mean.plan.list = len_q * g > kPagedFewRows && mean.list < std::min(mean.units, mean.spans);
+        c.apart = true;
+        c.many = mean.plan;
+    }
+    c.many.list = c.many.list && pages > 0;
+    return c;
 }
 
 // Wavefronts per token of norm_rope_kernel, each with as many of the token's groups of four head rows as the first (rounded up, so that

@@ -68,16 +68,11 @@ int64_t mx_area_pages(const pec_shape_t* shape, int32_t batch, int64_t total_q, 
 }
 
 // The sequences of the launch straight from their codes: units, or spans and their merge.
-int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, int64_t len_q, int64_t len_k, bool beside, char* ws,
+int mx_steps(const PagedAttnParams& p, const PagedMx& mx, const PagedLayout& l, int cu, const MxPlan& plan, int64_t len_q, int64_t len_k, char* ws,
              hipStream_t st) {
     using std::integral_constant;
     const int64_t batch = p.batch.batch, total_q = p.batch.total_q;
-    const int g = p.group;
-    MxPlan plan = mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch, total_q, len_q, len_k);
-    // Chunks `beside` sequences with few rows, of which len_k may be: units, unless few chunks may have a very long walk.  (24 steps on
-    // up to 42,000 keys with 2 prompts of 250: the prompts as units 55 us, as spans 120.)
-    if (beside && (len_k <= 16384 || total_q * g / (16 * plan.nt) * p.n_kv_heads >= cu / 4)) plan.units = true;
-    const int nt = plan.nt;
+    const int g = p.group, nt = plan.nt;
     // units of a KV head at most: of all packed rows, or of sequences that this launch is for
     int64_t row_tiles = total_q * g / (16 * nt) + batch;
     if (p.batch.most_q != 0) row_tiles = std::min(row_tiles, batch * (((int64_t)p.batch.most_q * g + 16 * nt - 1) / (16 * nt)));
@@ -232,24 +227,22 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const PagedLayout l = mx_layout(shape, batch->batch, batch->total_q, 0).paged;
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
-    // Chunks beside sequences with few rows: each kind by itself, in units that suit it (24 steps on up to 42,000 keys with 6 prompts of
-    // 1,100: all in units of 48 rows 252 us, the prompts in the area, below, 127).
-    const int few_q = std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g);
-    if (len_q > few_q && batch->batch - (batch->total_q + len_q - 1) / len_q > 2) {
+    const int64_t pages = l.capacity > 0 ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
+    const MxCall call = mx_call(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k, pages);
+    int64_t most = batch->batch;      // sequences that the area may be for
+    if (call.apart) {
         p.batch.least_q = 0;
-        p.batch.most_q = few_q;
-        if (int rc = mx_steps(p, mx, l, cu, few_q, len_k, false, ws, st)) return rc;
-        p.batch.least_q = few_q + 1;
+        p.batch.most_q = call.few_q;
+        if (int rc = mx_steps(p, mx, l, cu, mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, call.few_q, len_k), call.few_q,
+                              len_k, ws, st)) return rc;
+        p.batch.least_q = call.few_q + 1;
         p.batch.most_q = 0x7fffffff;
-        return mx_steps(p, mx, l, cu, len_q, len_k, true, ws, st);
+        most = std::min(most, batch->total_q / (call.few_q + 1));
     }
-    // Chunks by themselves: in the area, if it is there and that pays; what finds no room, if that can be, is left to the steps.
-    const int64_t pages = l.capacity > 0 && mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k).list
-                              ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
-    const bool list = pages > 0;
-    const bool room = batch->batch * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
+    // What finds no room in the area, if that can be, is left to the steps.
+    const bool room = most * (((int64_t)p.batch.max_keys + kMxAreaPage - 1) / kMxAreaPage) <= pages;
     MxAreaParams a{};
-    if (list) {
+    if (call.many.list) {
         const MxLayout m = mx_layout(shape, batch->batch, batch->total_q, pages);
         a.cache = mx;
         a.batch = p.batch;
@@ -265,11 +258,13 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
         if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
         p.batch.area = a.area;
     }
-    if (!list || !room) {
+    if (!call.many.list || !room) {
+        MxPlan plan = call.many;
+        if (call.apart && plan.list) plan.units = true;      // (few sequences or none: 25 with a chunk among them 5 us, as spans and their merge 40)
         p.batch.area_side = 0;
-        if (int rc = mx_steps(p, mx, l, cu, len_q, len_k, false, ws, st)) return rc;
+        if (int rc = mx_steps(p, mx, l, cu, plan, len_q, len_k, ws, st)) return rc;
     }
-    if (!list) return PEC_OK;
+    if (!call.many.list) return PEC_OK;
     const int64_t fill = std::min<int64_t>(pages * p.n_kv_heads, (int64_t)cu * 16);
     hipLaunchKernelGGL(paged_mx_fill_kernel, dim3((unsigned)fill), dim3(256), 0, st, a);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;

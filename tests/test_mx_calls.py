@@ -1,0 +1,36 @@
+"""How calls on a cache in 4 bits whose sequences differ are taken apart, and which of them keep their keys' way through the workspace."""
+from mx_calls import way
+
+STEPS = [(1, 3500)] * 24
+PROMPTS = [(1100, 1100), (900, 900), (600, 600), (700, 700), (1000, 1000), (800, 800)]
+
+
+def test_long_chunks_beside_steps_go_to_the_list():
+    assert way(32, 8, STEPS + [(512, 30512)], (512, 30512), 64, 477, 30512) == "steps, list"
+    assert way(32, 8, STEPS + [(512, 30512)], (512, 30512), 64, 477, 30512, spare_rows=40) == "steps, list"
+    assert way(32, 8, [(2, 3500)] * 24 + [(512, 30512)], (512, 30512), 64, 477, 30512) == "steps, list"
+    assert way(32, 8, STEPS + [(8192, 62500)], (8192, 62500), 64, 977, 62500) == "steps, list"
+    assert way(32, 8, [(1, 65000)] * 8 + [(8192, 60000)], (8192, 65000), 64, 1016, 60000) == "steps, list"
+    assert way(32, 8, STEPS + [(512, 30512)], (512, 30512), 64, 477) == "steps, units 3"      # no room
+
+
+def test_prompts_of_very_different_lengths_go_to_the_list():
+    for seqs in ([(16000, 16000)] + [(2000, 2000)] * 4, [(8192, 60000)] + [(1000, 30000)] * 7):
+        longest = max(t for _, t in seqs)
+        assert way(32, 8, seqs, (seqs[0][0], longest), 64, -(-longest // 64), sum(t for _, t in seqs)).endswith("list")
+    four = [(2048, 32000)] * 4
+    assert way(32, 8, four, (2048, 32000), 64, 500, 128000) == "list"
+    assert way(32, 8, four, (0, 0), 64, 500, 128000).endswith("list")
+
+
+def test_prompts_without_a_prefix_are_units():
+    """Whether a prefix of the longest sequence's length is theirs says the workspace."""
+    seqs = [(1, 2000 + 1700 * i) for i in range(24)] + PROMPTS
+    for room in (0, sum(t for _, t in PROMPTS)):
+        assert way(32, 8, seqs, (1100, 42000), 16, 2625, room) == "steps, units 3"
+    assert way(32, 8, STEPS + [(250, 250), (200, 200)], (250, 3500), 32, 110, 450) == "steps, units 3"
+
+
+def test_a_chunk_of_few_rows_behind_many_keys_is_spans():
+    for room in (0, 40000):
+        assert way(32, 8, STEPS + [(128, 40000)], (128, 40000), 32, 1250, room) == "steps, spans 3"
