@@ -449,7 +449,8 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
 // by themselves, each in units that suit them; `many` is the plan of the latter (of all sequences, if nothing is apart).  Its `list`:
 // their keys go to the area, `pages` pages of 64 keys that the workspace has room for, as far as they find it there.
 //
-// The longest have to leave room for more than two with few rows.  Of the sequences
+// Sequences of up to 48 rows, a unit, are one launch whatever their lengths (24 of 1 ... 5 tokens behind 10,000, 64 / 8 heads, 70 us, apart
+// 109).  Of others the longest have to leave room for more than two with few rows.  Of the sequences
 // with many rows the host knows the longest one's tokens and how many tokens there are: they are taken to be all that long, every
 // other sequence having one token.  Whether the longest one's keys are theirs it does not know, so the estimates without a prefix
 // and with one count alike, the latter with as many keys among them as one sequence can have, or as the area has room for: a
@@ -462,10 +463,11 @@ struct MxCall {
     bool apart;
     MxPlan many;
 };
+constexpr int kMxMostUnitRows = 48;
 inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, int64_t pages) {
     const int g = n_q_heads / n_kv_heads;
     MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, mx_plan(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k)};
-    if (len_q > c.few_q && batch - (total_q + len_q - 1) / len_q > 2) {
+    if (len_q > c.few_q && len_q * g > kMxMostUnitRows && batch - (total_q + len_q - 1) / len_q > 2) {
         const int64_t n = std::min(batch, std::max<int64_t>(1, (total_q - batch + (len_q - 1) / 2) / (len_q - 1)));
         const int64_t tokens = std::max(len_q, total_q - (batch - n));
         const int64_t prefix = std::max(len_q, pages > 0 ? std::min(len_k, 64 * pages / n) : len_k / n);
