@@ -450,14 +450,16 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
 // their keys go to the area, `pages` pages of 64 keys that the workspace has room for, as far as they find it there.
 //
 // Sequences of up to 48 rows, a unit, are one launch whatever their lengths (24 of 1 ... 5 tokens behind 10,000, 64 / 8 heads, 70 us, apart
-// 109).  Of others the longest have to leave room for more than two with few rows.  Of the sequences
+// 109).  Of others the longest have to leave room for more than two with few rows, and then the estimates decide.  Of the sequences
 // with many rows the host knows the longest one's tokens and how many tokens there are: they are taken to be all that long, every
 // other sequence having one token.  Whether the longest one's keys are theirs it does not know, so the estimates without a prefix
 // and with one count alike, the latter with as many keys among them as one sequence can have, or as the area has room for: a
 // workspace made for prompts that begin here (total_k) says that no long prefix is behind them.
 //
-// (512 tokens behind 30,000 beside 24 steps on 3,500, 32 / 8 heads, with room 298 us, straight from the codes 405; 8,192 behind 54,000
-// 5,910 / 8,110; 128 behind 40,000 180 in spans, 349 in units.)
+// After 200 calls of decode steps beside prompts and chunks, with room and without, each timed in one launch, and apart in units, in spans
+// and with the list: the choice costs 2 % on the mean, 42 % at most (always apart and never a list: 17 % on the mean).  (One launch / apart, 32 / 8
+// heads, beside 24 steps on 3,500: 512 tokens behind 30,000 385 / 299, 8,192 behind 54,000 8,350 / 6,110, 2 of 250 50 / 36; 79 tokens beside 45
+// steps on 385, 8 / 1 heads, 9 / 15.)
 struct MxCall {
     int few_q;
     bool apart;
@@ -466,7 +468,9 @@ struct MxCall {
 constexpr int kMxMostUnitRows = 48;
 inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, int64_t pages) {
     const int g = n_q_heads / n_kv_heads;
-    MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, mx_plan(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k)};
+    auto us = [&](const MxCost& c) { return c.plan.list && pages > 0 ? c.list : c.plan.units ? c.units : c.spans; };
+    const MxCost all = mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k);
+    MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, all.plan};
     if (len_q > c.few_q && len_q * g > kMxMostUnitRows && batch - (total_q + len_q - 1) / len_q > 2) {
         const int64_t n = std::min(batch, std::max<int64_t>(1, (total_q - batch + (len_q - 1) / 2) / (len_q - 1)));
         const int64_t tokens = std::max(len_q, total_q - (batch - n));
@@ -476,8 +480,11 @@ inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
         MxCost mean{with.plan, (with.units + none.units) / 2, (with.spans + none.spans) / 2, (with.list + none.list) / 2};
         mean.plan.units = mean.units <= mean.spans;
         mean.plan.list = len_q * g > kPagedFewRows && mean.list < std::min(mean.units, mean.spans);
-        c.apart = true;
-        c.many = mean.plan;
+        // without hints decode steps look like one long sequence: apart, and what is left over ends at once
+        const bool steps = total_q - batch < c.few_q;
+        if (steps) mean.plan.units = true, mean.plan.list = false;
+        c.apart = steps || us(mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, c.few_q, len_k)) + us(mean) <= us(all);
+        if (c.apart) c.many = mean.plan;
     }
     c.many.list = c.many.list && pages > 0;
     return c;

@@ -57,6 +57,8 @@ CASES = [      # heads, KV heads, page, hints, room, way
     (16, 2, 8, (150, 8000), 0, "steps, spans 3"),
     (12, 4, 16, (150, 8000), 0, "steps, units 3"),
     (32, 8, 16, (150, 0), 700, "steps, units 3"),
+    (8, 8, 16, (150, 8000), 0, "spans 3"),
+    (16, 2, 16, (150, 700), 0, "units 3"),
 ]
 
 
@@ -68,3 +70,10 @@ def test_ways(case):
     assert way(hq, hkv, b.seqs, hints, page, b.table.shape[1], room, 2) == want
     for causal in (True, False):
         check(b, ref, hints, room, causal)
+
+
+def test_decode_steps_without_hints():
+    seqs = [(1, 1 + 37 * i % 800) for i in range(70)]
+    b = MxBatch(52, 8, 2, 16, seqs, spare_rows=0, table_extra=600)
+    assert way(8, 2, seqs, (0, 0), 16, b.table.shape[1]) == "steps, units 3"
+    check(b, {True: attention(b)}, (0, 0), 0)

@@ -33,7 +33,7 @@ def test_prompts_without_a_prefix_are_units():
 
 def test_a_chunk_of_few_rows_behind_many_keys_is_spans():
     for room in (0, 40000):
-        assert way(32, 8, STEPS + [(128, 40000)], (128, 40000), 32, 1250, room) == "steps, spans 3"
+        assert way(32, 8, STEPS + [(128, 40000)], (128, 40000), 32, 1250, room) == "spans 3"
 
 
 def test_sequences_of_a_unit_each_are_one_launch():
@@ -41,3 +41,14 @@ def test_sequences_of_a_unit_each_are_one_launch():
     assert way(64, 8, [(5, 10000)] * 24, (5, 10000), 32, 313) == "spans 3"
     assert way(32, 8, [(1 + i % 9, 10000) for i in range(24)], (9, 10000), 32, 313, 60000) == "spans 3"
     assert way(64, 8, [(1, 540)] * 4, (0, 0), 16, 34) == "units 2"
+
+
+def test_short_calls_are_one_launch():
+    assert way(8, 1, [(1, 385)] * 45 + [(79, 79)], (79, 385), 16, 25, 79) == "units 3"
+    assert way(10, 2, [(5, 60)] * 7 + [(71, 147)] * 5, (71, 147), 16, 10, 500) == "units 3"
+
+
+def test_decode_steps_without_hints_leave_nothing_over():
+    assert way(32, 8, [(1, 8000)] * 64, (0, 0), 16, 500) == "steps, units 3"
+    assert way(32, 8, [(1, 8000)] * 64, (0, 0), 16, 500, 100000) == "steps, units 3"
+    assert way(32, 8, [(1, 60000)] * 64, (0, 0), 16, 3750) == "steps, units 3"
