@@ -181,7 +181,8 @@ int launch_paged_list(const PagedAttnParams& p, const PagedLayout& l, int cu, in
     w.work = reinterpret_cast<WorkItem*>(ws + l.off_work);
     w.counters = reinterpret_cast<int32_t*>(ws + l.off_counters);
     w.splits = reinterpret_cast<PagedSplit*>(ws + l.off_splits);
-    hipLaunchKernelGGL(paged_list_kernel, dim3(1), dim3(1024), 0, st, w);
+    if (p.batch.area) hipLaunchKernelGGL(paged_list_kernel<true>, dim3(1), dim3(1024), 0, st, w);
+    else hipLaunchKernelGGL(paged_list_kernel<false>, dim3(1), dim3(1024), 0, st, w);
     if (hipGetLastError() != hipSuccess) return PEC_ERR_HIP;
     FwdParams f{};
     f.q = p.q;

@@ -41,23 +41,25 @@ struct PagedBatch {
     const int32_t* table;        // [batch][table_len]
     int32_t batch, table_len, total_q;
     int32_t max_keys;            // table_len pages, at most 2^30 keys
-    // of a cache in 4 bits, or null: where a sequence's keys are in bf16 as well, first page, or -1; the launch is for those
-    // sequences (area_side 1) or for the others (0), which to the other launch are without queries
+    // Of a cache in 4 bits, whose calls may have several launches, each for some of the sequences (paged_seq<true>).  Or null: where a
+    // sequence's keys are in bf16 as well, first page, or -1; the launch is for those sequences (area_side 1) or for the others (0)
     const int32_t* area;
     int32_t area_side;
-    int32_t least_q, most_q;     // if most_q is not 0, the launch is for sequences with so many new tokens, and the others are without queries
+    int32_t least_q, most_q;     // if most_q is not 0, the launch is for sequences with so many new tokens
 };
 
 struct PagedSeq {
     int32_t q0, len_q, len_k;
 };
+// SOME: the launch is for some of the sequences, and the others are without queries.
+template <bool SOME = false>
 __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& b, int i) {
     PagedSeq s;
     s.q0 = min(max(b.cu_q[i], 0), b.total_q);
     s.len_q = min(max(b.cu_q[i + 1], s.q0), b.total_q) - s.q0;
     s.len_k = min(max(b.len_k[i], 0), b.max_keys);
-    if (b.area && (b.area[i] >= 0 ? 1 : 0) != b.area_side) s.len_q = 0;
-    if (b.most_q != 0 && (s.len_q < b.least_q || s.len_q > b.most_q)) s.len_q = 0;
+    if (SOME && b.area && (b.area[i] >= 0 ? 1 : 0) != b.area_side) s.len_q = 0;
+    if (SOME && b.most_q != 0 && (s.len_q < b.least_q || s.len_q > b.most_q)) s.len_q = 0;
     return s;
 }
 

@@ -54,6 +54,8 @@ struct PagedTiles {
 // Keys per range, as the smallest of sixteen estimates, one per wavefront; 0x40000000: no tile is cut.  In tile steps of 64
 // keys: an item takes 8 besides its own (its first loads, its results), its partial results 4 more, and their merge with its
 // launch 8 per call; items that are all alike run in whole rounds, others even out but for half an item at the end.
+// SOME: of sequences in the area of a call on a cache in 4 bits, whose pages there take the place of their row of the block table.
+template <bool SOME>
 __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams p) {
     struct Seq {
         PagedSeq s;
@@ -71,14 +73,14 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
 
     // ---- the longest walk, then the estimates.  Up to 1,024 sequences are read once and stay in LDS.
     const bool held = bt.batch <= kPagedListSeqs;
-    auto seq_at = [&](int b) { return held ? seqs[b].s : paged_seq(bt, b); };
+    auto seq_at = [&](int b) { return held ? seqs[b].s : paged_seq<SOME>(bt, b); };
     // Lanes that share a sequence: of up to 64, as many as a wavefront has for each; above, one.
     int log_per = 0;
     while (bt.batch << log_per << 1 <= 64) ++log_per;
     const int per = 1 << log_per, sub = lane & (per - 1), mine = lane >> log_per;
     int longest = 0;
     for (int b = tid; b < bt.batch; b += 1024) {
-        const PagedSeq s = paged_seq(bt, b);
+        const PagedSeq s = paged_seq<SOME>(bt, b);
         if (held) seqs[b].s = s;
         const PagedTiles t(s, p);
         if (t.n > 0) longest = max(longest, t.keys(t.n - 1));
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
     // ---- items of sequence `b`, from place `pos0` of the list on: range by range, the last tile first
     auto place = [&](int b, const PagedSeq& sq, int pos0) {
         const PagedTiles t(sq, p);
-        const int table_row = bt.area ? bt.area[b] : b;
+        const int table_row = SOME ? bt.area[b] : b;
         for (int tile = lane; tile < t.n; tile += 64) {
             const int keys = t.keys(tile), n_ranges = max(1, (int)(((int64_t)keys + range - 1) / range));
             int slot0 = -1;
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(const PagedListParams 
         const int b = c0 + tid;
         if (b >= bt.batch) return;
         Seq q;
-        q.s = held ? seqs[tid].s : paged_seq(bt, b);
+        q.s = held ? seqs[tid].s : paged_seq<SOME>(bt, b);
         const PagedTiles t(q.s, p);
         q.n_items = t.n > 0 ? t.items(range, 0, 1) : 0;
         seqs[tid] = q;

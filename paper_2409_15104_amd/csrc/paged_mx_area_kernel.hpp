@@ -42,7 +42,7 @@ __global__ __launch_bounds__(1024) void paged_mx_area_kernel(const MxAreaParams 
         int pages = 0;
         bool many = false;
         if (b < p.batch.batch) {
-            const PagedSeq s = paged_seq(p.batch, b);
+            const PagedSeq s = paged_seq<true>(p.batch, b);
             many = s.len_q > 0;
             pages = many ? (s.len_k + kMxAreaPage - 1) / kMxAreaPage : 0;
         }

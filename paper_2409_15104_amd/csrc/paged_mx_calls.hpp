@@ -38,7 +38,7 @@ int check_cache_mx(const pec_shape_t* s, const pec_paged_cache_mx_t* c, PagedMx*
 
 // Whether neighbouring heads' rows of a token are neighbours in memory: 64 bytes each, half a cache line.
 bool mx_by_token(const PagedMx& mx) { return mx.head_b < mx.row_b; }
-constexpr int kMxStepRows = 48;      // of a slot of a partial result, at most
+constexpr int kMxStepRows = kMxMostUnitRows;      // of a slot of a partial result, at most
 // Spans of all KV heads: one for every wavefront of eight to a compute unit at most, and one for every head at least.
 int mx_most_spans(int cu, int n_kv_heads) { return std::max((cu & ~7) * 8, (n_kv_heads + 63) / 64 * 64); }
 // Workspace of pec_attn_paged_mx: pec_attn_paged's, then the area (paged_mx_area_kernel.hpp) of so many pages.

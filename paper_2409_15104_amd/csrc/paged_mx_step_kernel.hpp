@@ -42,6 +42,7 @@ __device__ __forceinline__ int least_span_mx(int total, int longest, int n_kv_he
 
 // How a call's sequences are cut: R = 16, 32 or 48 rows a unit; as StepCut.
 struct MxCut {
+    static constexpr bool kSome = true;
     FastDiv group, rows;
     int causal;
     __device__ __forceinline__ int tile_of(int row) const { return rows.div(row); }
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
     const PagedBatch& bt = p.a.batch;
 
     auto length = [&](const PagedSeq& s) { return UNITS ? cut.row_tiles(s) : cut.all_tiles(s); };
-    PagedLine<HEADS * WAVES, decltype(length)> line(bt, length, chunk_sum, wave_no);
+    PagedLine<HEADS * WAVES, true, decltype(length)> line(bt, length, chunk_sum, wave_no);
     if (!UNITS && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
         for (int ch = wave_no, ahead = 0, at = 0; ch < line.n_chunks; ch += HEADS * WAVES) {
             for (; at < ch; ++at) ahead = add_up(ahead, chunk_sum[at]);

@@ -44,6 +44,7 @@ __device__ __forceinline__ int add_up(int x, int y) { return (int)min((uint32_t)
 
 // How a call's sequences are cut: R = 2^log_r rows a unit; a sequence has less than 2^31 rows.
 struct StepCut {
+    static constexpr bool kSome = false;
     FastDiv group;
     int log_r, causal, most_rows;
     __device__ __forceinline__ int tile_of(int row) const { return row >> log_r; }
@@ -68,6 +69,7 @@ struct StepCut {
 };
 template <class Cut>
 struct PagedStepParamsOf {
+    static constexpr bool kSome = Cut::kSome;      // whether a launch may be for some of the sequences
     PagedAttnParams a;
     float* part_out;          // [spans][KV heads][2][32 NT][128]
     float* part_lse;          // [spans][KV heads][2][32 NT]
@@ -111,7 +113,7 @@ __device__ __forceinline__ int least_span(int total, int longest, int n_kv_heads
 
 // Sequences laid end to end, `value` of a sequence being its length on that line.  Up to 64 of them sit in the lanes of every
 // wavefront; of more, `chunk_sum` (LDS) keeps the sums of 64 at a time, which the wavefronts share out among themselves.
-template <int WAVES, class Value>
+template <int WAVES, bool SOME, class Value>
 struct PagedLine {
     const PagedBatch& bt;
     const Value value;
@@ -121,7 +123,7 @@ struct PagedLine {
     int own, upto, total;
     __device__ __forceinline__ PagedSeq load(int b) const {
         PagedSeq s{0, 0, 0};
-        if (b < bt.batch) s = paged_seq(bt, b);
+        if (b < bt.batch) s = paged_seq<SOME>(bt, b);
         return s;
     }
     __device__ __forceinline__ PagedLine(const PagedBatch& batch, Value v, int32_t* sums, int wave)
@@ -150,7 +152,7 @@ struct PagedLine {
             s.len_q = __builtin_amdgcn_readlane(lanes.len_q, i);
             s.len_k = __builtin_amdgcn_readlane(lanes.len_k, i);
         } else {
-            s = paged_seq(bt, i);
+            s = paged_seq<SOME>(bt, i);
             s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
             s.len_q = __builtin_amdgcn_readfirstlane(s.len_q);
             s.len_k = __builtin_amdgcn_readfirstlane(s.len_k);
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void paged_step_kernel(const PagedSt
     auto length = [&](const PagedSeq& s) {
         return SHARED ? cut.row_tiles(s) : cut.all_tiles(s);
     };
-    PagedLine<WAVES, decltype(length)> line(bt, length, chunk_sum, wave);
+    PagedLine<WAVES, false, decltype(length)> line(bt, length, chunk_sum, wave);
     if (!SHARED && blockIdx.x == 0) {       // steps of a KV head ahead of every sequence, for the merge
         for (int c = wave, ahead = 0, at = 0; c < line.n_chunks; c += WAVES) {
             for (; at < c; ++at) ahead = add_up(ahead, chunk_sum[at]);
@@ -691,7 +693,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_merge_ker
     constexpr int PER_GROUP = WAVES == 1 ? 4 : 1;       // rows a workgroup works on at a time
     for (int x = blockIdx.x * PER_GROUP + (WAVES == 1 ? (int)(threadIdx.x >> 6) : 0); x < bt.batch * tokens; x += gridDim.x * PER_GROUP) {
         const int seq = x / tokens;
-        const PagedSeq s = paged_seq(bt, seq);
+        const PagedSeq s = paged_seq<Params::kSome>(bt, seq);
         const int before = p.prefix[seq], n_rt = p.cut.row_tiles(s);
         if (per_head == 0 || n_rt == 0) continue;
         const StepSpans spans(per_head, p.n_spans, least);
