@@ -432,8 +432,10 @@ typedef struct {
  * bf16, and v rounded to codes.  A group of 32 dims whose largest magnitude is m 2^E, 1 <= m < 2, takes the scale 2^(E - 2), or 2^(E - 1)
  * where m >= 1.75, kept between 2^-125 and 2^125; values are rounded to the nearest code, ties to the even one, what is beyond 6
  * to 6.  A group that holds NaN or an infinity is NaN (byte 255, codes 0).  What an element comes back as is off by at most
- * a fifth of it, or by 0.25 x scale, which is 1/14 of the group's largest magnitude at most.  Of two tokens of a call that go to the
- * same slot (sequences that share a page) the codes of one and the scales of the other may be what stays there.
+ * a fifth of it, or by 0.25 x scale; this is at most 1/14 of the group's largest magnitude, if that is 3.5 x 2^-125 or more (below,
+ * the scale stays 2^-125), and where it is 7 x 2^125 and more, values beyond 6 x 2^125 are off by up to a quarter.  Of
+ * two tokens of a call that go to the same slot (sequences that share a page) the codes of one and the scales of the other may be
+ * what stays there.
  */
 int pec_paged_append_mx(const pec_shape_t* shape, const pec_norm_rope_t* norm_rope, const pec_paged_cache_mx_t* cache,
                         const pec_paged_batch_t* batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
