@@ -736,7 +736,8 @@ def pec_paged_mx_workspace_bytes(n_q_heads: int, n_kv_heads: int, batch: int, to
 def pec_attn_paged_mx(q, cache: PagedCacheMx, block_table, cu_seqlens_q, seqlens_k, max_len_q: int = 0, max_len_k: int = 0,
                       causal: bool = True, out_dtype=torch.bfloat16, scale: float = 0.0, flags: int = 0, out=None, lse=None,
                       workspace=None, total_k: int = 0, stream=None):
-    """pec_attn_paged over a cache in 4 bits.  total_k: keys that a workspace made here has room for (see pec_paged_mx_workspace_bytes)."""
+    """pec_attn_paged over a cache in 4 bits.  total_k: keys of sequences with many new tokens, the sum of their seqlens_k, that a
+    workspace made here has room for (see pec_attn.h): without it chunks behind long prefixes take half as long again."""
     index, sizes = cache.index, q.shape
     q_stride = _rows(q, "q", index)
     total, hq = sizes[0], sizes[1]

@@ -449,7 +449,7 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
 // by themselves, each in units that suit them; `many` is the plan of the latter (of all sequences, if nothing is apart).  Its `list`:
 // their keys go to the area, `pages` pages of 64 keys that the workspace has room for, as far as they find it there.
 //
-// Sequences of up to 48 rows, a unit, are one launch whatever their lengths (24 of 1 ... 5 tokens behind 10,000, 64 / 8 heads, 70 us, apart
+// Sequences of up to 48 rows, a unit, are one launch whatever their lengths (24 of 1 ... 5 tokens behind 10,000, 64 / 8 heads, 66 us, apart
 // 109).  Of others the longest have to leave room for more than two with few rows, and then the estimates decide.  Of the sequences
 // with many rows the host knows the longest one's tokens and how many tokens there are: they are taken to be all that long, every
 // other sequence having one token.  Whether the longest one's keys are theirs it does not know, so the estimates without a prefix

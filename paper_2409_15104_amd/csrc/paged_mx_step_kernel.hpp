@@ -20,9 +20,11 @@
 // Weights are rounded to bf16 once, for their product with the values, as everywhere here; scores, sums, results and their merge are fp32.
 //
 // What bounds it: by heads memory, 4 sequences of 107,500 tokens, 64 / 8 heads (488 MB) 85 us with the merge, 120 of 3,300, 32 / 8 (435
-// MB) 90, 5.0 TB/s while the spans run, where the loads alone take 82; by token half cache lines, 105 us for the former.  24 x 5 drafted tokens on
-// 10,350, 64 / 8 heads, 48 rows: instructions, 270 of the vector ALU and 48 matrix products for a tile, 83 us by heads, 89 by token.  640 new
-// tokens behind 1,000, 32 / 8, in units: 27 us.  4 of 540 in units: 8 us, latency.
+// MB) 89, 5.2 TB/s while the spans run, where the loads alone take 82; by token half cache lines, 105 us for the former.  24 x 5 drafted tokens on
+// 10,350, 64 / 8 heads, 48 rows: 81 us by heads, 89 by token, two wavefronts to a SIMD, each a chain of products, softmax, conversions
+// and products.  270 instructions of the vector ALU and 48 matrix products for a tile keep the one busy for half of the time and the other
+// for 28 %; of a wavefront's time 30 % goes for data that are not there and 31 % for its turn.  640 new tokens behind 1,000, 32 / 8, in
+// units: 27 us.  4 of 540 in units: 8 us, latency.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -209,7 +211,9 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
     uint32_t v_lane[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v_lane[i] = (4u * (SMALL ? c & 1 : c) + i) * cache.row_b + 4u * m;
-    // Codes that no other wavefront wants are marked as read once; half a cache line is left for the neighbouring head's.
+    // Codes are marked as read once, but where heads share a workgroup and half a cache line is left for the neighbouring one's.  (By heads
+    // 4 x 107,500 tokens 85 us, without the mark 94; it is on codes that are read again, too, by token with 32 and 48 rows by the
+    // neighbouring head's workgroup, 24 x 5 drafted tokens 89 / 91, and by other units of a prompt, 3 of 640 32.0 / 31.2.)
     auto code_load = [](auto* from) {
         if constexpr (HEADS > 1) return *from;
         else return __builtin_nontemporal_load(from);
