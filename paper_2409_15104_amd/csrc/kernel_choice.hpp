@@ -446,7 +446,7 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
 }
 
 // A call on a cache in 4 bits as a whole.  `apart`: sequences with few rows, up to few_q new tokens, and those with many are launched
-// by themselves, each in units that suit them; `many` is the plan of the latter (of all sequences, if nothing is apart).  Its `list`:
+// by themselves, each in units that suit them; `few` and `many` are their plans (`many` that of all sequences, if nothing is apart).  `list`:
 // their keys go to the area, `pages` pages of 64 keys that the workspace has room for, as far as they find it there.
 //
 // Sequences of up to 48 rows, a unit, are one launch whatever their lengths (24 of 1 ... 5 tokens behind 10,000, 64 / 8 heads, 66 us, apart
@@ -463,14 +463,18 @@ inline MxPlan mx_plan(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
 struct MxCall {
     int few_q;
     bool apart;
-    MxPlan many;
+    MxPlan few, many;
 };
 constexpr int kMxMostUnitRows = 48;
-inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int64_t total_q, int64_t len_q, int64_t len_k, int64_t pages) {
+inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t places, int64_t total_q, int64_t max_len_q, int64_t len_k, int64_t pages) {
     const int g = n_q_heads / n_kv_heads;
+    const bool known = max_len_q > 0 && max_len_q < total_q;
+    const int64_t len_q = known ? max_len_q : total_q;
+    // sequences with new tokens, at most: a token of each besides the longest one's (places of a batch may be empty)
+    const int64_t batch = known ? std::min(places, total_q - len_q + 1) : places;
     auto us = [&](const MxCost& c) { return c.plan.list && pages > 0 ? c.list : c.plan.units ? c.units : c.spans; };
     const MxCost all = mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, len_q, len_k);
-    MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, all.plan};
+    MxCall c{std::max(1, (g <= 16 ? 16 : g <= 32 ? 32 : 64) / g), false, {}, all.plan};
     if (len_q > c.few_q && len_q * g > kMxMostUnitRows && batch - (total_q + len_q - 1) / len_q > 2) {
         const int64_t n = std::min(batch, std::max<int64_t>(1, (total_q - batch + (len_q - 1) / 2) / (len_q - 1)));
         const int64_t tokens = std::max(len_q, total_q - (batch - n));
@@ -481,10 +485,11 @@ inline MxCall mx_call(int cu, int n_q_heads, int n_kv_heads, int64_t batch, int6
         mean.plan.units = mean.units <= mean.spans;
         mean.plan.list = len_q * g > kPagedFewRows && mean.list < std::min(mean.units, mean.spans);
         // without hints decode steps look like one long sequence: apart, and what is left over ends at once
-        const bool steps = total_q - batch < c.few_q;
+        const bool steps = !known && total_q - batch < c.few_q;
         if (steps) mean.plan.units = true, mean.plan.list = false;
-        c.apart = steps || us(mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, c.few_q, len_k)) + us(mean) <= us(all);
-        if (c.apart) c.many = mean.plan;
+        const MxCost few = mx_cost(cu, n_q_heads, n_kv_heads, batch, total_q, c.few_q, len_k);
+        c.apart = steps || us(few) + us(mean) <= us(all);
+        if (c.apart) c.few = few.plan, c.many = mean.plan;
     }
     c.many.list = c.many.list && pages > 0;
     return c;

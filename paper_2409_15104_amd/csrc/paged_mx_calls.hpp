@@ -228,13 +228,12 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
     const int64_t pages = l.capacity > 0 ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
-    const MxCall call = mx_call(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, len_q, len_k, pages);
+    const MxCall call = mx_call(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, batch->max_len_q, len_k, pages);
     int64_t most = batch->batch;      // sequences that the area may be for
     if (call.apart) {
         p.batch.least_q = 0;
         p.batch.most_q = call.few_q;
-        if (int rc = mx_steps(p, mx, l, cu, mx_plan(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, call.few_q, len_k), call.few_q,
-                              len_k, ws, st)) return rc;
+        if (int rc = mx_steps(p, mx, l, cu, call.few, call.few_q, len_k, ws, st)) return rc;
         p.batch.least_q = call.few_q + 1;
         p.batch.most_q = 0x7fffffff;
         most = std::min(most, batch->total_q / (call.few_q + 1));

@@ -14,6 +14,12 @@ def test_long_chunks_beside_steps_go_to_the_list():
     assert way(32, 8, STEPS + [(512, 30512)], (512, 30512), 64, 477) == "steps, units 3"      # no room
 
 
+def test_places_of_a_batch_that_are_empty_change_nothing():
+    for empty in (10, 1000):
+        assert way(32, 8, STEPS + [(512, 30512)] + [(0, 0)] * empty, (512, 30512), 64, 477, 30512) == "steps, list"
+    assert way(32, 8, [(512, 30512)] + [(0, 0)] * 10, (512, 30512), 64, 477, 30512).endswith("list")
+
+
 def test_prompts_of_very_different_lengths_go_to_the_list():
     for seqs in ([(16000, 16000)] + [(2000, 2000)] * 4, [(8192, 60000)] + [(1000, 30000)] * 7):
         longest = max(t for _, t in seqs)
@@ -52,3 +58,4 @@ def test_decode_steps_without_hints_leave_nothing_over():
     assert way(32, 8, [(1, 8000)] * 64, (0, 0), 16, 500) == "steps, units 3"
     assert way(32, 8, [(1, 8000)] * 64, (0, 0), 16, 500, 100000) == "steps, units 3"
     assert way(32, 8, [(1, 60000)] * 64, (0, 0), 16, 3750) == "steps, units 3"
+    assert way(32, 8, [(1, 60000)] * 64, (512, 60000), 16, 3750, 100000) == "steps, units 3"      # a bound in the place of the longest
