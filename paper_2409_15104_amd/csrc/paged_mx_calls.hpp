@@ -227,7 +227,8 @@ int pec_attn_paged_mx(const pec_shape_t* shape, const pec_paged_cache_mx_t* cach
     const PagedLayout l = mx_layout(shape, batch->batch, batch->total_q, 0).paged;
     char* const ws = static_cast<char*>(workspace);
     const int64_t len_k = batch->max_len_k > 0 ? std::min<int64_t>(batch->max_len_k, p.batch.max_keys) : p.batch.max_keys;
-    const int64_t pages = l.capacity > 0 ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
+    const bool may_list = l.capacity > 0 && l.capacity * l.units <= 0x7fffffff;      // (launch_paged_list's limit)
+    const int64_t pages = may_list ? mx_area_pages(shape, batch->batch, batch->total_q, workspace_bytes) : 0;
     const MxCall call = mx_call(cu, p.n_q_heads, p.n_kv_heads, batch->batch, batch->total_q, batch->max_len_q, len_k, pages);
     int64_t most = batch->batch;      // sequences that the area may be for
     if (call.apart) {

@@ -471,7 +471,7 @@ __global__ __launch_bounds__(HEADS * WAVES * 64, 2) void paged_mx_step_kernel(co
                         if (at_key > last_vis[x]) continue;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            __builtin_amdgcn_sched_barrier(0);
+                            __builtin_amdgcn_sched_barrier(0);      // (four values at a time: registers are short)
                             const u32x4 y = mx_values(codes[i], scale);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
